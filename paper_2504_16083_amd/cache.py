@@ -1,0 +1,305 @@
+"""ctypes binding of include/mmi_cache.h: rotary positions, the paged cache and
+the attention of drafted tokens over it.
+
+As in mmi.py the functions have the C names and marshal arguments only; what
+the C side cannot see (types, shapes and devices of the tensors) is checked
+here with ValueError, the rest by the library (MMIError). Tensors are torch
+device tensors on the context's device; their strides are passed on, the last
+dimension must be contiguous. Work goes to `stream`, or to the device's
+current stream."""
+from __future__ import annotations
+
+import ctypes as ct
+import math
+
+import torch
+
+from . import mmi
+from .mmi import _check
+
+D = 128
+LAYOUTS = {"half": 0, "interleaved": 1}
+SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
+TYPES = {"bf16": 0, "fp8": 1, "int8": 2, "fp4": 3}
+ROW_BYTES = {"bf16": 256, "fp8": 128, "int8": 128, "fp4": 64}
+
+
+class mmi_rope_cfg(ct.Structure):
+    _fields_ = [("rot_dim", ct.c_int32), ("layout", ct.c_int32), ("scaling", ct.c_int32), ("inverse", ct.c_int32),
+                ("sections", ct.c_int32 * 3), ("reserved", ct.c_int32),
+                ("theta", ct.c_double), ("factor", ct.c_double), ("orig_len", ct.c_double),
+                ("beta_fast", ct.c_double), ("beta_slow", ct.c_double), ("attn_factor", ct.c_double),
+                ("inv_freq", ct.POINTER(ct.c_double))]
+
+
+class mmi_cache(ct.Structure):
+    _fields_ = [("type", ct.c_int32), ("page", ct.c_int32), ("Hkv", ct.c_int32), ("D", ct.c_int32),
+                ("n_pages", ct.c_int64), ("k", ct.c_void_p), ("v", ct.c_void_p),
+                ("k_scale", ct.c_void_p), ("v_scale", ct.c_void_p),
+                ("page_stride", ct.c_int64), ("scale_stride", ct.c_int64)]
+
+
+class mmi_tree(ct.Structure):
+    _fields_ = [("n_seq", ct.c_int32), ("n_rows", ct.c_int32), ("Hq", ct.c_int32), ("max_rows", ct.c_int32),
+                ("max_len", ct.c_int64), ("max_pages", ct.c_int32), ("mask_words", ct.c_int32),
+                ("row_start", ct.c_void_p), ("length", ct.c_void_p), ("pages", ct.c_void_p), ("mask", ct.c_void_p),
+                ("q_stride_s", ct.c_int64), ("q_stride_h", ct.c_int64),
+                ("k_stride_s", ct.c_int64), ("k_stride_h", ct.c_int64),
+                ("v_stride_s", ct.c_int64), ("v_stride_h", ct.c_int64),
+                ("o_stride_s", ct.c_int64), ("o_stride_h", ct.c_int64),
+                ("scale", ct.c_float), ("reserved", ct.c_int32)]
+
+
+SYMBOLS = ["mmi_rope", "mmi_cache_write", "mmi_cache_read", "mmi_tree_workspace", "mmi_tree_attention"]
+
+_lib = None
+
+
+def lib():
+    global _lib
+    if _lib is None:
+        L = mmi.lib()
+        vp, i64, sz, P = ct.c_void_p, ct.c_int64, ct.c_size_t, ct.POINTER
+        sig = {
+            "mmi_rope": [vp, P(mmi.mmi_problem), P(mmi_rope_cfg), vp, vp, vp, vp, vp, vp],
+            "mmi_cache_write": [vp, P(mmi_cache), vp, i64, i64, vp, i64, i64, vp, i64, vp],
+            "mmi_cache_read": [vp, P(mmi_cache), vp, i64, vp, i64, i64, vp, i64, i64, vp],
+            "mmi_tree_workspace": [vp, P(mmi_cache), P(mmi_tree), P(sz)],
+            "mmi_tree_attention": [vp, P(mmi_cache), P(mmi_tree), vp, vp, vp, vp, vp, vp, sz, vp],
+        }
+        for name, args in sig.items():
+            f = getattr(L, name)
+            f.argtypes, f.restype = args, ct.c_int
+        _lib = L
+    return _lib
+
+
+def _stream(ctx, stream):
+    if stream is None:
+        stream = torch.cuda.current_stream(ctx.device)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _rows(ctx, name, t, n, heads):
+    """A [n, heads, 128] bfloat16 tensor on the context's device; its strides."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[2] != D:
+        raise ValueError(f"{name} must be a bfloat16 tensor [tokens, heads, {D}]")
+    if (n is not None and t.shape[0] != n) or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, [{n}, {heads}, {D}] expected")
+    if t.device.type != "cuda" or t.device.index != ctx.device:
+        raise ValueError(f"{name} is on {t.device}, the context on device {ctx.device}")
+    ss, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    # torch leaves the stride of a dimension of one entry open
+    if t.shape[1] == 1:
+        sh = D
+    if t.shape[0] <= 1:
+        ss = max(sh * t.shape[1], D)
+    return ss, sh
+
+
+def _array(ctx, name, t, dtype, shape):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    if t.device.type != "cuda" or t.device.index != ctx.device:
+        raise ValueError(f"{name} is on {t.device}, the context on device {ctx.device}")
+    return t.data_ptr()
+
+
+# ------------------------------------------------------------------ rotary positions
+class RopeCfg:
+    """Rotation of the first rot_dim channels (mmi_rope_cfg). layout: "half"
+    (pair i = channels i, i + rot_dim / 2) or "interleaved" (2i, 2i + 1);
+    scaling: "none", "linear", "ntk" or "parts"; sections: pairs that take
+    their position from the t, h and w axis; attn_factor 0: the default of the
+    scaling; inv_freq: radians a position of every pair, in place of theta and
+    the scaling."""
+
+    def __init__(self, rot_dim=128, layout="half", theta=10000.0, scaling="none", factor=1.0, orig_len=0.0,
+                 beta_fast=32.0, beta_slow=1.0, attn_factor=0.0, sections=(0, 0, 0), inv_freq=None):
+        if layout not in LAYOUTS or scaling not in SCALINGS:
+            raise ValueError(f"layout {layout!r} or scaling {scaling!r} is unknown")
+        if len(sections) != 3:
+            raise ValueError("sections are three numbers of pairs")
+        self.axes = 3 if any(sections) else 1
+        table = None
+        if inv_freq is not None:
+            if len(inv_freq) != rot_dim // 2:
+                raise ValueError(f"{len(inv_freq)} frequencies for {rot_dim // 2} pairs")
+            table = (ct.c_double * max(1, len(inv_freq)))(*[float(f) for f in inv_freq])
+        self._table = table
+        self.c = [mmi_rope_cfg(rot_dim, LAYOUTS[layout], SCALINGS[scaling], inverse, (ct.c_int32 * 3)(*sections), 0,
+                               theta, factor, orig_len, beta_fast, beta_slow, attn_factor, table)
+                  for inverse in (0, 1)]
+
+
+def mmi_rope(ctx, cfg, q=None, k=None, pos=None, q_out=None, k_out=None, inverse=False, stream=None):
+    """Rotates q [S, Hq, 128] and k [S, Hkv, 128] (either may be None), in place
+    unless q_out / k_out are given (strides as the inputs'). pos: int32 [S], or
+    [3, S] with sections; None: 0 .. S-1. inverse: the gradient's rotation."""
+    if q is None and k is None:
+        raise ValueError("neither q nor k")
+    p = mmi.mmi_problem()
+    p.S = (q if q is not None else k).shape[0]
+    p.D, p.block, p.Hq, p.Hkv = D, 64, 1, 1
+    if k is not None:
+        p.k_stride_s, p.k_stride_h = strides = _rows(ctx, "k", k, p.S, None)
+        p.Hkv = k.shape[1]
+        if k_out is None:
+            k_out = k
+        elif _rows(ctx, "k_out", k_out, p.S, p.Hkv) != strides:
+            raise ValueError("k_out must have the strides of k")
+        p.Hq = p.Hkv
+    if q is not None:
+        p.q_stride_s, p.q_stride_h = strides = _rows(ctx, "q", q, p.S, None)
+        p.Hq = q.shape[1]
+        if k is None:
+            p.Hkv = 1
+        if q_out is None:
+            q_out = q
+        elif _rows(ctx, "q_out", q_out, p.S, p.Hq) != strides:
+            raise ValueError("q_out must have the strides of q")
+    pp = None
+    if pos is not None:
+        pp = _array(ctx, "pos", pos, torch.int32, (p.S,) if cfg.axes == 1 else (3, p.S))
+    _check(lib().mmi_rope(ctx.h, ct.byref(p), ct.byref(cfg.c[1 if inverse else 0]), pp,
+                          None if q is None else q.data_ptr(), None if k is None else k.data_ptr(),
+                          None if q is None else q_out.data_ptr(), None if k is None else k_out.data_ptr(),
+                          _stream(ctx, stream)))
+
+
+# ------------------------------------------------------------------ the cache
+class Cache:
+    """The memory of a paged cache (mmi_cache). k, v: [n_pages, Hkv, page, 128]
+    bfloat16 for type "bf16", else uint8 [n_pages, Hkv, page, bytes a row]
+    (128 for "fp8" and "int8", 64 for "fp4") with k_scale, v_scale uint8
+    [n_pages, Hkv, page, 4]; only the first dimension may be strided."""
+
+    def __init__(self, type, k, v, k_scale=None, v_scale=None):
+        if type not in TYPES:
+            raise ValueError(f"cache type {type!r} is unknown")
+        self.type, self.k, self.v, self.k_scale, self.v_scale = type, k, v, k_scale, v_scale
+        self.n_pages, self.Hkv, self.page = k.shape[:3]
+        want = (self.n_pages, self.Hkv, self.page)
+        bf16 = type == "bf16"
+        self.device = k.device
+        row = D if bf16 else ROW_BYTES[type]
+        stride = self._pool("k", k, torch.bfloat16 if bf16 else torch.uint8, want + (row,))
+        if self._pool("v", v, torch.bfloat16 if bf16 else torch.uint8, want + (row,)) != stride:
+            raise ValueError("k and v must have the same strides")
+        scale = 0
+        if not bf16:
+            if k_scale is None or v_scale is None:
+                raise ValueError(f"a cache of type {type!r} has scales")
+            scale = self._pool("k_scale", k_scale, torch.uint8, want + (4,))
+            if self._pool("v_scale", v_scale, torch.uint8, want + (4,)) != scale:
+                raise ValueError("k_scale and v_scale must have the same strides")
+        else:
+            self.k_scale = self.v_scale = None
+        self.c = mmi_cache(TYPES[type], self.page, self.Hkv, D, self.n_pages, k.data_ptr(), v.data_ptr(),
+                           None if bf16 else k_scale.data_ptr(), None if bf16 else v_scale.data_ptr(),
+                           stride * (2 if bf16 else 1), scale)
+
+    def _pool(self, name, t, dtype, shape):
+        if t.dtype != dtype or tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be a {dtype} tensor of shape {shape}")
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, k on {self.device}")
+        if math.prod(shape) and not t[0].is_contiguous():
+            raise ValueError(f"the pages of {name} must be contiguous")
+        return t.stride(0) if shape[0] > 1 else 0
+
+    @classmethod
+    def empty(cls, type, n_pages, Hkv, page, device=0):
+        """A cache of this size, its memory zeroed."""
+        if type not in TYPES:
+            raise ValueError(f"cache type {type!r} is unknown")
+        dev = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
+        if type == "bf16":
+            return cls(type, *(torch.zeros(n_pages, Hkv, page, D, dtype=torch.bfloat16, device=dev) for _ in "kv"))
+        return cls(type, *(torch.zeros(n_pages, Hkv, page, n, dtype=torch.uint8, device=dev)
+                           for n in (ROW_BYTES[type], ROW_BYTES[type], 4, 4)))
+
+
+def _on(ctx, cache):
+    if cache.device.type != "cuda" or cache.device.index != ctx.device:
+        raise ValueError(f"the cache is on {cache.device}, the context on device {ctx.device}")
+
+
+def mmi_cache_write(ctx, cache, k, v, slot, stream=None):
+    """Rows i of k and v [n, Hkv, 128] into slot[i] (int64 [n], page number *
+    page + place; outside the cache: nowhere)."""
+    _on(ctx, cache)
+    n = k.shape[0]
+    ks, vs = _rows(ctx, "k", k, n, cache.Hkv), _rows(ctx, "v", v, n, cache.Hkv)
+    _check(lib().mmi_cache_write(ctx.h, ct.byref(cache.c), k.data_ptr(), *ks, v.data_ptr(), *vs,
+                                 _array(ctx, "slot", slot, torch.int64, (n,)), n, _stream(ctx, stream)))
+
+
+def mmi_cache_read(ctx, cache, slot, k, v, stream=None):
+    """Rows i of k and v [n, Hkv, 128] = what slot[i] holds (outside: zeros)."""
+    _on(ctx, cache)
+    n = k.shape[0]
+    ks, vs = _rows(ctx, "k", k, n, cache.Hkv), _rows(ctx, "v", v, n, cache.Hkv)
+    _check(lib().mmi_cache_read(ctx.h, ct.byref(cache.c), _array(ctx, "slot", slot, torch.int64, (n,)), n,
+                                k.data_ptr(), *ks, v.data_ptr(), *vs, _stream(ctx, stream)))
+
+
+# ------------------------------------------------------------------ drafted tokens
+class Tree:
+    """A batch of sequences with drafted tokens (mmi_tree): row_start int32
+    [n_seq + 1], length int32 [n_seq] (cached tokens), pages int32 [n_seq,
+    max_pages], mask int64 [n_rows, words] (bit j of a row: it sees drafted
+    token j; None: token i sees 0 .. i), max_rows and max_len the most drafted
+    and cached tokens of a sequence. The tensors' contents may change between
+    calls, within these bounds."""
+
+    def __init__(self, row_start, length, pages, mask=None, max_rows=1, max_len=0, scale=0.0):
+        self.row_start, self.length, self.pages, self.mask = row_start, length, pages, mask
+        self.max_rows, self.max_len, self.scale = max_rows, max_len, scale
+
+    def _struct(self, ctx, Hq, n_rows):
+        t = mmi_tree()
+        t.n_seq, t.n_rows, t.Hq, t.max_rows, t.max_len = self.length.shape[0], n_rows, Hq, self.max_rows, self.max_len
+        t.row_start = _array(ctx, "row_start", self.row_start, torch.int32, (t.n_seq + 1,))
+        t.length = _array(ctx, "length", self.length, torch.int32, (t.n_seq,))
+        if self.pages.dim() != 2:
+            raise ValueError("pages must be a tensor [n_seq, max_pages]")
+        t.max_pages = self.pages.shape[1]
+        t.pages = _array(ctx, "pages", self.pages, torch.int32, (t.n_seq, t.max_pages))
+        if self.mask is not None:
+            if self.mask.dim() != 2:
+                raise ValueError("mask must be a tensor [n_rows, words]")
+            t.mask_words = self.mask.shape[1]
+            t.mask = _array(ctx, "mask", self.mask, torch.int64, (n_rows, t.mask_words))
+        t.scale = self.scale
+        return t
+
+
+def mmi_tree_workspace(ctx, cache, tree, Hq, n_rows) -> int:
+    """Bytes of workspace of a batch with these bounds."""
+    need = ct.c_size_t()
+    _check(lib().mmi_tree_workspace(ctx.h, ct.byref(cache.c), ct.byref(tree._struct(ctx, Hq, n_rows)),
+                                    ct.byref(need)))
+    return need.value
+
+
+def mmi_tree_attention(ctx, cache, tree, q, k, v, o, workspace, lse=None, stream=None):
+    """o [n_rows, Hq, 128] = attention of the drafted tokens' rows q over their
+    sequences' cached tokens and the drafted k, v [n_rows, Hkv, 128]; lse:
+    float32 [Hq, n_rows] or None; workspace: uint8 of mmi_tree_workspace bytes,
+    not shared with a call that may run at the same time."""
+    _on(ctx, cache)
+    n = q.shape[0]
+    qs = _rows(ctx, "q", q, None, None)
+    Hq = q.shape[1]
+    t = tree._struct(ctx, Hq, n)
+    t.q_stride_s, t.q_stride_h = qs
+    t.k_stride_s, t.k_stride_h = _rows(ctx, "k", k, n, cache.Hkv)
+    t.v_stride_s, t.v_stride_h = _rows(ctx, "v", v, n, cache.Hkv)
+    t.o_stride_s, t.o_stride_h = _rows(ctx, "o", o, n, Hq)
+    lp = None if lse is None else _array(ctx, "lse", lse, torch.float32, (Hq, n))
+    wp = _array(ctx, "workspace", workspace, torch.uint8, (workspace.numel(),))
+    _check(lib().mmi_tree_attention(ctx.h, ct.byref(cache.c), ct.byref(t), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                    o.data_ptr(), lp, wp, workspace.numel(), _stream(ctx, stream)))

@@ -1,0 +1,578 @@
+// Attention of drafted tokens over the paged cache (include/mmi_cache.h).
+//
+// The query rows of a KV head are (drafted token, query head of its group):
+// row r of sequence b is token r / g, head r % g. A workgroup takes a tile of
+// 32 of them and a chunk of the sequence's cached tokens; the last chunk also
+// takes the drafted tokens. Its four waves split the keys: each takes every
+// fourth block of 32 keys, stages it in LDS of its own (no barriers in the
+// loop) as bfloat16 whatever the cache's type, and keeps an online softmax:
+//   S^T (32 keys x 32 rows) = K Q^T           8 MFMA 32x32x16 bf16
+//   P = 2^(S - m), running maximum m and sums in fp32
+//   O^T (128 x 32) += V^T P^T                 8 MFMA 32x32x16 bf16
+// S^T has one row a lane, so its maximum and sum are in-lane but for one
+// exchange of halves, and P is already the operand of the second product.
+// At the end the waves' O, m and sums meet in LDS; a sequence of several
+// chunks leaves partials that k_tree_join merges in a fixed order.
+#include <algorithm>
+
+#include "cache.hpp"
+#include "codec.hpp"
+
+namespace mmi {
+
+constexpr int KB = 32;                 // keys of a block
+constexpr int TK = 136, TV = 160;      // bf16 a staged K / V row: operand reads without bank conflicts
+constexpr int OP = 132;                // floats a row of the join buffer
+constexpr float SLACK = 8.0f;          // the maximum moves when a block's passes it by this (log2 units)
+constexpr int CHUNK = 128;             // chunks are multiples of a step of the four waves
+
+struct __align__(16) WaveTile {
+  uint16_t k[KB * TK];
+  uint16_t v[KB * TV];
+};
+
+typedef __attribute__((address_space(3))) bf16x4 lds4;
+
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
+
+struct Seq {
+  int row0, T, L;                      // first row, drafted tokens, cached tokens
+};
+
+__device__ __forceinline__ Seq sequence(const TreeArgs& a, int b) {
+  Seq s;
+  s.row0 = clampi(a.row_start[b], 0, a.n_rows);
+  s.T = clampi(a.row_start[b + 1], s.row0, min(a.n_rows, s.row0 + a.max_rows)) - s.row0;
+  s.L = clampi(a.length[b], 0, a.max_len);
+  return s;
+}
+
+// Between one lane's LDS accesses and another's of the same wave: the wave's
+// are done in order, the compiler must keep that order.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Sum over the workgroup's 256 threads, and the sum before this thread.
+__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* before, int64_t* sh) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t s = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up(s, d);
+    if (lane >= d) s += y;
+  }
+  __syncthreads();
+  if (lane == 63) sh[wave] = s;
+  __syncthreads();
+  int64_t base = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) base += sh[w];
+    all += sh[w];
+  }
+  *before = base + s - x;
+  return all;
+}
+
+struct Item {
+  int b, first, chunks, chunk, tile, head;   // sequence, its first item, its chunks; this one's chunk, tile, head
+  int c0, c1;                                // cached tokens
+};
+
+// Item `it` of the batch. The chunk length follows from the work of the whole
+// batch (cached tokens x tiles x heads, cut into `target` parts), so long
+// sequences get many chunks and short ones few, whatever the bounds were.
+template <int ROWS>
+__device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, int64_t* sh64, int* sh) {
+  const int tid = threadIdx.x;
+  int64_t work = 0, before;
+  for (int b = tid; b < a.n_seq; b += 256) {
+    const Seq s = sequence(a, b);
+    work += (int64_t)((s.T * a.g + ROWS - 1) / ROWS) * s.L;
+  }
+  work = block_scan(work, &before, sh64) * a.c.Hkv;
+  const int64_t len = (work + a.target - 1) / a.target;
+  const int chunk = (int)((max(len, (int64_t)1) + CHUNK - 1) / CHUNK * CHUNK);
+  if (tid == 0) sh[0] = -1;
+  int64_t base = 0;
+  for (int b0 = 0; b0 < a.n_seq; b0 += 256) {
+    const int b = b0 + tid;
+    Seq s = {0, 0, 0};
+    if (b < a.n_seq) s = sequence(a, b);
+    const int tiles = (s.T * a.g + ROWS - 1) / ROWS, chunks = max(1, (s.L + chunk - 1) / chunk);
+    const int64_t n = (int64_t)tiles * a.c.Hkv * chunks;
+    const int64_t all = block_scan(n, &before, sh64);
+    const int64_t at = it - base - before;
+    if (n > 0 && at >= 0 && at < n) {
+      const int tile = (int)(at % tiles), head = (int)(at / tiles % a.c.Hkv);
+      const int c = (int)(at / ((int64_t)tiles * a.c.Hkv));
+      sh[0] = b; sh[1] = (int)(base + before); sh[2] = chunks; sh[3] = c; sh[4] = tile; sh[5] = head;
+      sh[6] = min(s.L, c * chunk);
+      sh[7] = (int)min((int64_t)s.L, (int64_t)(c + 1) * chunk);
+      if (at == 0) {
+        a.rec[2 * b] = it;
+        a.rec[2 * b + 1] = chunks;
+      }
+    }
+    base += all;
+    if (base > it) break;
+  }
+  __syncthreads();
+  r.b = __builtin_amdgcn_readfirstlane(sh[0]);
+  r.first = __builtin_amdgcn_readfirstlane(sh[1]);
+  r.chunks = __builtin_amdgcn_readfirstlane(sh[2]);
+  r.chunk = __builtin_amdgcn_readfirstlane(sh[3]);
+  r.tile = __builtin_amdgcn_readfirstlane(sh[4]);
+  r.head = __builtin_amdgcn_readfirstlane(sh[5]);
+  r.c0 = __builtin_amdgcn_readfirstlane(sh[6]);
+  r.c1 = __builtin_amdgcn_readfirstlane(sh[7]);
+  return r.b >= 0;
+}
+
+// A block of 32 cached keys in registers, as its 16-byte pieces lie in the
+// cache: piece i of a lane belongs to key i * RP + lane / CPR.
+template <int TYPE>
+struct Raw {
+  static constexpr int CPR = Codec<TYPE>::ROW / 16;   // pieces a row
+  static constexpr int RP = 64 / CPR;                 // rows a wave-wide load
+  static constexpr int N = KB / RP;
+  u32x4 k[N], v[N];
+  uint32_t ks[N], vs[N];
+  uint32_t seen;                                      // keys that exist
+};
+
+template <int TYPE>
+__device__ __forceinline__ void load_block(Raw<TYPE>& r, const TreeArgs& a, const int32_t* pages, int head, int t0,
+                                           int len, int lane) {
+  typedef Raw<TYPE> R;
+  r.seen = len - t0 >= KB ? 0xffffffffu : (1u << (len - t0)) - 1;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {              // 16 keys lie in one page
+    const int t = t0 + 16 * half;
+    const int p = t < len ? pages[t >> a.c.shift] : -1;
+    const bool ok = (uint32_t)p < (uint64_t)a.c.n_pages;
+    if (!ok) r.seen &= half ? 0x0000ffffu : 0xffff0000u;
+    const int64_t page = ok ? p : 0;
+    const int64_t in = ((int64_t)head << a.c.shift) + (t & ((1 << a.c.shift) - 1));
+    const uint8_t* kp = a.c.k + page * a.c.page_stride + in * Codec<TYPE>::ROW;
+    const uint8_t* vp = a.c.v + page * a.c.page_stride + in * Codec<TYPE>::ROW;
+    const uint32_t* ksp = Codec<TYPE>::SCALED ? (const uint32_t*)((const uint8_t*)a.c.ks + page * a.c.scale_stride) + in : nullptr;
+    const uint32_t* vsp = Codec<TYPE>::SCALED ? (const uint32_t*)((const uint8_t*)a.c.vs + page * a.c.scale_stride) + in : nullptr;
+#pragma unroll
+    for (int i = half * R::N / 2; i < (half + 1) * R::N / 2; ++i) {
+      const int row = (i - half * R::N / 2) * R::RP + lane / R::CPR;
+      const int off = row * Codec<TYPE>::ROW + lane % R::CPR * 16;
+      r.k[i] = *reinterpret_cast<const u32x4*>(kp + off);
+      r.v[i] = *reinterpret_cast<const u32x4*>(vp + off);
+      if constexpr (Codec<TYPE>::SCALED) {
+        r.ks[i] = ksp[row];
+        r.vs[i] = vsp[row];
+      }
+    }
+  }
+}
+
+// One 16-byte piece as bfloat16 into a staged row.
+template <int TYPE>
+__device__ __forceinline__ void put_piece(uint16_t* to, u32x4 w, uint32_t scales, int piece) {
+  if constexpr (TYPE == MMI_CACHE_BF16) {
+    *reinterpret_cast<u32x4*>(to + piece * 8) = w;
+  } else {
+    const float s = scale_value(scales >> (TYPE == MMI_CACHE_FP4 ? 8 * piece : 8 * (piece >> 1)) & 255);
+    if constexpr (TYPE == MMI_CACHE_FP4) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<bf16x8*>(to + piece * 32 + 8 * e) = decode4(w[e], s);
+    } else {
+      *reinterpret_cast<bf16x8*>(to + piece * 16) = decode8<TYPE>(w[0], w[1], s);
+      *reinterpret_cast<bf16x8*>(to + piece * 16 + 8) = decode8<TYPE>(w[2], w[3], s);
+    }
+  }
+}
+
+template <int TYPE>
+__device__ __forceinline__ void stage_block(WaveTile& t, const Raw<TYPE>& r, int lane) {
+  typedef Raw<TYPE> R;
+#pragma unroll
+  for (int i = 0; i < R::N; ++i) {
+    const int row = i * R::RP + lane / R::CPR, piece = lane % R::CPR;
+    put_piece<TYPE>(&t.k[row * TK], r.k[i], r.ks[i], piece);
+    // a key that does not exist weighs nothing, whatever its place in the page holds
+    const bool ok = r.seen >> row & 1;
+    const u32x4 none = {};
+    put_piece<TYPE>(&t.v[row * TV], ok ? r.v[i] : none, ok ? r.vs[i] : 0u, piece);
+  }
+}
+
+// Bits of the eight bfloat16 in w that are an infinity or a NaN, as a word of
+// eight flags; `keep` gets w with those set to zero.
+__device__ __forceinline__ bool not_finite(u32x4 w, u32x4& keep) {
+  bool any = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bool lo = (w[e] & 0x7f80u) == 0x7f80u, hi = (w[e] & 0x7f800000u) == 0x7f800000u;
+    any |= lo | hi;
+    keep[e] = (lo ? 0u : w[e] & 0xffffu) | (hi ? 0u : w[e] & 0xffff0000u);
+  }
+  return any;
+}
+
+struct Rows {                          // a wave's 32 rows
+  f32x16 o[4];
+  bf16x8 q[8];
+  float m, l, lo;                      // running maximum (log2 units), sums of the fp32 and of the bf16 P
+};
+
+__device__ __forceinline__ float half_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ float half_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ bf16x8 v_operand(const WaveTile& t, int vlane, int half, int dt) {
+  const uint16_t* p = &t.v[vlane + 16 * half * TV + 32 * dt];
+  const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p));
+  const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p + 8 * TV));
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// The staged block against the wave's rows; bit k of `seen`: this lane's row
+// sees key k.
+__device__ __forceinline__ void attend(Rows& r, const WaveTile& t, uint32_t seen, float sc, int c, int h, int vlane) {
+  f32x16 s = {};
+#pragma unroll
+  for (int x = 0; x < 8; ++x)
+    s = mfma32(*reinterpret_cast<const bf16x8*>(&t.k[c * TK + h * 64 + x * 8]), r.q[x], s);
+  if (__any(seen != 0xffffffffu)) {
+    const uint32_t mine = seen >> (4 * h);   // element 4 i + j is key 8 i + 4 h + j
+#pragma unroll
+    for (int x = 0; x < 16; ++x)
+      if (!(mine >> (8 * (x >> 2) + (x & 3)) & 1)) s[x] = -INFINITY;
+  }
+  float mx = s[0];
+#pragma unroll
+  for (int x = 1; x < 16; ++x) mx = fmaxf(mx, s[x]);
+  mx = half_max(mx) * sc;                  // sc > 0
+  if (__any(mx > r.m + SLACK)) {
+    const float m = fmaxf(r.m, mx), alpha = r.m == m ? 1.0f : fast_exp2(r.m - m);
+    r.m = m;
+    r.l *= alpha;
+    r.lo *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) r.o[dt][x] *= alpha;
+  }
+  const float base = r.m == -INFINITY ? 0.0f : r.m;   // nothing seen yet: every P below is 2^-inf = 0
+  float rs = 0.0f, ro = 0.0f;
+  bf16x8 p[2];
+#pragma unroll
+  for (int x = 0; x < 16; ++x) {
+    const float e = fast_exp2(fmaf(s[x], sc, -base));
+    rs += e;
+    const __bf16 b = (__bf16)e;            // rounded for the product; O is divided by the sum of these
+    p[x >> 3][x & 7] = b;
+    ro += (float)b;
+  }
+  r.l += half_sum(rs);
+  r.lo += half_sum(ro);
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) r.o[dt] = mfma32(v_operand(t, vlane, half, dt), p[half], r.o[dt]);
+}
+
+// Infinities and NaN in the V of drafted keys reach only the rows that see
+// them (a product over the block would spread them as 0 x inf): the block was
+// staged without them, and here what they add is found from products of 0/1
+// flags, of the rows that see a key and of the channels where it holds +inf,
+// -inf or a NaN. v: V of the block's first key, n: its keys.
+__device__ __forceinline__ void add_not_finite(f32x16 (&o)[4], WaveTile& t, const uint16_t* v, int64_t ss, int n,
+                                               uint32_t seen, int h, int vlane, int lane) {
+  bf16x8 flag[2];
+#pragma unroll
+  for (int x = 0; x < 16; ++x)
+    flag[x >> 3][x & 7] = (__bf16)((seen >> (8 * (x >> 2) + 4 * h + (x & 3)) & 1) ? 1.0f : 0.0f);
+  for (int what = 0; what < 3; ++what) {   // +inf, -inf, NaN
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const u32x4 raw = *reinterpret_cast<const u32x4*>(v + (int64_t)min(4 * i + lane / 16, n - 1) * ss + lane % 16 * 8);
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t f = 0;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const uint32_t u = raw[e] >> (16 * s) & 0xffff;
+          const bool hit = what == 2 ? (u & 0x7fff) > 0x7f80 : u == (what ? 0xff80u : 0x7f80u);
+          f |= hit ? 0x3f80u << (16 * s) : 0u;
+        }
+        w[e] = f;
+      }
+      *reinterpret_cast<u32x4*>(&t.v[(4 * i + lane / 16) * TV + lane % 16 * 8]) = w;
+    }
+    wave_fence();
+    const float add = what == 2 ? __uint_as_float(0x7fc00000u) : what ? -INFINITY : INFINITY;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) {
+      f32x16 n = {};
+#pragma unroll
+      for (int half = 0; half < 2; ++half) n = mfma32(v_operand(t, vlane, half, dt), flag[half], n);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) o[dt][x] += n[x] > 0.0f ? add : 0.0f;
+    }
+    wave_fence();
+  }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_tree(TreeArgs a) {
+  constexpr int ROWS = 32;
+  __shared__ WaveTile tiles[4];
+  __shared__ float ml[4][ROWS][4];
+  __shared__ int64_t sh64[4];
+  __shared__ int sh[8];
+  Item it;
+  if (!find_item<ROWS>(a, blockIdx.x, it, sh64, sh)) return;
+  const Seq sq = sequence(a, it.b);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int c = lane & 31, h = lane >> 5;
+  WaveTile& t = tiles[wave];
+  // transpose-read source of this lane inside a staged V block: in each
+  // 16-lane group, output lane i, element e is element i % 4 of the 8 bytes
+  // addressed by lane 4 e + i / 4
+  const int grp = lane >> 4, li = lane & 15;
+  const int vlane = (4 * (grp >> 1) + (li >> 2)) * TV + 16 * (grp & 1) + 4 * (li & 3);
+
+  Rows r;
+  const int row = it.tile * ROWS + c, tok = row / a.g;
+  const bool live = tok < sq.T;
+  {
+    const uint16_t* q = (const uint16_t*)a.q.p + (int64_t)(sq.row0 + (live ? tok : 0)) * a.q.ss +
+                        (int64_t)(it.head * a.g + (live ? row - tok * a.g : 0)) * a.q.sh + h * 64;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const bf16x8 y = load16(q + 8 * x);
+      r.q[x] = live ? y : zero8();
+    }
+  }
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) r.o[dt][x] = 0.0f;
+  r.m = -INFINITY;
+  r.l = r.lo = 0.0f;
+
+  const int32_t* pages = a.pages + (int64_t)it.b * a.max_pages;
+  Raw<TYPE> raw;
+  int t0 = it.c0 + KB * wave;
+  if (t0 < it.c1) load_block<TYPE>(raw, a, pages, it.head, t0, it.c1, lane);
+  for (; t0 < it.c1; t0 += 4 * KB) {
+    const uint32_t seen = raw.seen;
+    stage_block<TYPE>(t, raw, lane);
+    if (t0 + 4 * KB < it.c1) load_block<TYPE>(raw, a, pages, it.head, t0 + 4 * KB, it.c1, lane);
+    wave_fence();
+    attend(r, t, seen, a.sc, c, h, vlane);
+    wave_fence();
+  }
+  if (it.chunk == it.chunks - 1) {
+    const uint16_t* kb = (const uint16_t*)a.k.p + (int64_t)sq.row0 * a.k.ss + (int64_t)it.head * a.k.sh;
+    const uint16_t* vb = (const uint16_t*)a.v.p + (int64_t)sq.row0 * a.v.ss + (int64_t)it.head * a.v.sh;
+    for (int d0 = KB * wave; d0 < sq.T; d0 += 4 * KB) {
+      u32x4 kr[8], vr[8];
+      uint64_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int d = min(d0 + 4 * i + lane / 16, sq.T - 1);
+        kr[i] = *reinterpret_cast<const u32x4*>(kb + (int64_t)d * a.k.ss + lane % 16 * 8);
+        vr[i] = *reinterpret_cast<const u32x4*>(vb + (int64_t)d * a.v.ss + lane % 16 * 8);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = 4 * i + lane / 16;
+        u32x4 keep;
+        odd |= __ballot(not_finite(vr[i], keep));
+        const u32x4 none = {};
+        *reinterpret_cast<u32x4*>(&t.k[key * TK + lane % 16 * 8]) = kr[i];
+        *reinterpret_cast<u32x4*>(&t.v[key * TV + lane % 16 * 8]) = d0 + key < sq.T ? keep : none;
+      }
+      uint32_t seen = sq.T - d0 >= KB ? 0xffffffffu : (1u << (sq.T - d0)) - 1;
+      if (a.mask) {
+        const uint32_t* mr = a.mask + (int64_t)(sq.row0 + min(tok, sq.T - 1)) * (2 * a.mask_words);
+        seen &= mr[d0 >> 5];
+      } else {
+        const int n = tok + 1 - d0;        // keys d0 .. tok
+        seen &= n >= KB ? 0xffffffffu : n > 0 ? (1u << n) - 1 : 0u;
+      }
+      wave_fence();
+      attend(r, t, seen, a.sc, c, h, vlane);
+      wave_fence();
+      if (odd) add_not_finite(r.o, t, vb + (int64_t)d0 * a.v.ss, a.v.ss, sq.T - d0, seen, h, vlane, lane);
+    }
+  }
+
+  // the waves' parts of each row, weighed by their maxima
+  if (h == 0) {
+    ml[wave][c][0] = r.m;
+    ml[wave][c][1] = r.lo;
+    ml[wave][c][2] = r.l;
+  }
+  __syncthreads();                         // also: the staged blocks are done with
+  float* buf = reinterpret_cast<float*>(tiles) + wave * ROWS * OP;
+  static_assert(sizeof(tiles) >= 4 * ROWS * OP * sizeof(float), "the join buffer lies in the tiles");
+  {
+    float m = ml[0][c][0];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, ml[w][c][0]);
+    const float f = r.m == -INFINITY ? 0.0f : fast_exp2(r.m - m);
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(buf + c * OP + 32 * dt + 8 * i + 4 * h) =
+            make_float4(r.o[dt][4 * i] * f, r.o[dt][4 * i + 1] * f, r.o[dt][4 * i + 2] * f, r.o[dt][4 * i + 3] * f);
+  }
+  __syncthreads();
+  const int jr = tid >> 3, part = tid & 7;               // row of the tile, 16 channels
+  const int jrow = it.tile * ROWS + jr, jtok = jrow / a.g;
+  if (jtok >= sq.T) return;
+  float m = ml[0][jr][0];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) m = fmaxf(m, ml[w][jr][0]);
+  float l = 0.0f, lo = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = ml[w][jr][0] == -INFINITY ? 0.0f : fast_exp2(ml[w][jr][0] - m);
+    lo += ml[w][jr][1] * f;
+    l += ml[w][jr][2] * f;
+  }
+  float o[16];
+#pragma unroll
+  for (int x = 0; x < 16; ++x) o[x] = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(tiles) + (w * ROWS + jr) * OP +
+                                                        part * 16 + 4 * x);
+      o[4 * x] += y.x; o[4 * x + 1] += y.y; o[4 * x + 2] += y.z; o[4 * x + 3] += y.w;
+    }
+  if (it.chunks == 1) {
+    const float inv = lo > 0.0f ? 1.0f / lo : lo == 0.0f ? 0.0f : lo;   // no key seen: 0; NaN stays
+    const int head = it.head * a.g + jrow - jtok * a.g;
+    uint16_t* to = a.o + (int64_t)(sq.row0 + jtok) * a.o_ss + (int64_t)head * a.o_sh + part * 16;
+    bf16x8 y[2];
+#pragma unroll
+    for (int x = 0; x < 16; ++x) y[x >> 3][x & 7] = (__bf16)(o[x] * inv);
+    *reinterpret_cast<bf16x8*>(to) = y[0];
+    *reinterpret_cast<bf16x8*>(to + 8) = y[1];
+    if (a.lse && part == 0)
+      a.lse[(int64_t)head * a.n_rows + sq.row0 + jtok] = l == 0.0f ? -INFINITY : (m + fast_log2(l)) * LN2;
+  } else {
+    const int64_t at = (int64_t)blockIdx.x * ROWS + jr;
+    float* to = a.part_o + at * D + part * 16;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *reinterpret_cast<float4*>(to + 4 * x) = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+    if (part == 0) *reinterpret_cast<float4*>(a.part_ml + at * 4) = make_float4(m, lo, l, 0.0f);
+  }
+}
+
+// Joins the partials of the sequences that were cut into chunks. Workgroup
+// (row of a sequence's rows, KV head and sequence): 8 groups of 32 lanes take
+// every eighth partial, 4 channels a lane, and meet in LDS.
+template <int ROWS>
+__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
+  const int rows = a.max_rows * a.g, row = blockIdx.x % rows;
+  const int head = blockIdx.x / rows % a.c.Hkv, b = blockIdx.x / rows / a.c.Hkv;
+  const Seq sq = sequence(a, b);
+  const int tok = row / a.g;
+  if (tok >= sq.T) return;
+  const int first = a.rec[2 * b], chunks = a.rec[2 * b + 1];
+  if (chunks <= 1) return;
+  const int tiles = (sq.T * a.g + ROWS - 1) / ROWS;
+  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
+  auto slot = [&](int p) {
+    return ((int64_t)first + ((int64_t)p * a.c.Hkv + head) * tiles + row / ROWS) * ROWS + row % ROWS;
+  };
+  __shared__ float4 so[8][32];
+  __shared__ float sm[8][3];
+  float m = -INFINITY;
+  for (int p = grp; p < chunks; p += 8) m = fmaxf(m, a.part_ml[slot(p) * 4]);
+  if (lane == 0) sm[grp][0] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) m = fmaxf(m, sm[w][0]);
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float l = 0.0f, lo = 0.0f;
+  for (int p = grp; p < chunks; p += 8) {
+    const float4 e = *reinterpret_cast<const float4*>(a.part_ml + slot(p) * 4);
+    const float4 y = *reinterpret_cast<const float4*>(a.part_o + slot(p) * D + 4 * lane);
+    const float f = e.x == -INFINITY ? 0.0f : fast_exp2(e.x - m);
+    lo += e.y * f;
+    l += e.z * f;
+    o.x += y.x * f; o.y += y.y * f; o.z += y.z * f; o.w += y.w * f;
+  }
+  so[grp][lane] = o;
+  __syncthreads();
+  if (lane == 0) { sm[grp][1] = lo; sm[grp][2] = l; }
+  __syncthreads();
+  if (grp) return;
+#pragma unroll
+  for (int w = 1; w < 8; ++w) {
+    const float4 y = so[w][lane];
+    o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
+    lo += sm[w][1];
+    l += sm[w][2];
+  }
+  const float inv = lo > 0.0f ? 1.0f / lo : lo == 0.0f ? 0.0f : lo;
+  const int qh = head * a.g + row - tok * a.g;
+  uint16_t* to = a.o + (int64_t)(sq.row0 + tok) * a.o_ss + (int64_t)qh * a.o_sh + 4 * lane;
+  bf16x4 y = {(__bf16)(o.x * inv), (__bf16)(o.y * inv), (__bf16)(o.z * inv), (__bf16)(o.w * inv)};
+  *reinterpret_cast<bf16x4*>(to) = y;
+  if (a.lse && lane == 0)
+    a.lse[(int64_t)qh * a.n_rows + sq.row0 + tok] = l == 0.0f ? -INFINITY : (m + fast_log2(l)) * LN2;
+}
+
+TreeShape tree_shape(const mmi_tree& t, int Hkv, int cus) {
+  TreeShape s{};
+  const int g = t.Hq / Hkv;
+  s.rows = 32;
+  s.target = 2 * cus;
+  // tiles of all sequences, and `target` chunks more (each sequence's last chunk may be short)
+  const int64_t most = (t.max_rows * (int64_t)g + s.rows - 1) / s.rows;
+  const int64_t tiles = std::min<int64_t>(most * t.n_seq, ((int64_t)t.n_rows * g + (int64_t)t.n_seq * (s.rows - 1)) / s.rows);
+  const int64_t items = tiles * Hkv + s.target;
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  const int64_t limit = (int64_t)1 << 22;
+  if (items > limit || (int64_t)t.max_rows * t.Hq * t.n_seq > 2 * limit) throw Error(MMI_ERR_UNSUPPORTED, "the batch is cut into more than 2^22 workgroups");
+  s.items = (int32_t)items;
+  s.part_o = 0;
+  s.part_ml = up((size_t)items * s.rows * D * 4);
+  s.rec = s.part_ml + up((size_t)items * s.rows * 16);
+  s.bytes = s.rec + up((size_t)t.n_seq * 8);
+  return s;
+}
+
+hipError_t launch_tree(const TreeArgs& a, int type, int rows, hipStream_t st) {
+  if (a.n_seq <= 0 || a.n_rows <= 0) return hipSuccess;
+  const dim3 grid((unsigned)a.items);
+  switch (type) {
+    case MMI_CACHE_BF16: hipLaunchKernelGGL(k_tree<MMI_CACHE_BF16>, grid, dim3(256), 0, st, a); break;
+    case MMI_CACHE_FP8: hipLaunchKernelGGL(k_tree<MMI_CACHE_FP8>, grid, dim3(256), 0, st, a); break;
+    case MMI_CACHE_INT8: hipLaunchKernelGGL(k_tree<MMI_CACHE_INT8>, grid, dim3(256), 0, st, a); break;
+    case MMI_CACHE_FP4: hipLaunchKernelGGL(k_tree<MMI_CACHE_FP4>, grid, dim3(256), 0, st, a); break;
+    default: return hipErrorInvalidValue;
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.max_len <= CHUNK) return e;   // one chunk a sequence at most
+  hipLaunchKernelGGL(k_tree_join<32>, dim3((unsigned)(a.max_rows * a.g * a.c.Hkv * a.n_seq)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace mmi

@@ -1,7 +1,7 @@
 // Host runtime of libmmi: argument validation, modality layout, the plan
 // (estimation jobs, choices, permutations, block index, work list), launch
 // sequencing on the caller's stream, a caching device allocator, and the
-// C entry points declared in include/mmi.h.
+// C entry points declared in include/mmi.h and include/mmi_cache.h.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -16,6 +16,7 @@
 #include <functional>
 #include <vector>
 
+#include "cache.hpp"
 #include "device.hpp"
 #include "internal.hpp"
 
@@ -1599,6 +1600,86 @@ int mmi_search(mmi_ctx* ctx, const mmi_problem* prob, const void* q, const void*
     const mmi_problem p = normalise(prob);
     HIPCHK(hipSetDevice(ctx->device));
     search_layer(ctx, p, q, k, v, cands, n_cands, xc, n_xc, *target, (hipStream_t)stream, out, report);
+  });
+}
+
+// --------------------------------------------- operators around the prefill (mmi_cache.h)
+// The context's device for the time of a call, then the caller's again.
+struct OnDevice {
+  int was = -1;
+  explicit OnDevice(int device) {
+    HIPCHK(hipGetDevice(&was));
+    if (was == device) was = -1;
+    else HIPCHK(hipSetDevice(device));
+  }
+  ~OnDevice() {
+    if (was >= 0) (void)hipSetDevice(was);
+  }
+};
+
+int mmi_rope(mmi_ctx* ctx, const mmi_problem* prob, const mmi_rope_cfg* cfg, const int32_t* pos, const void* q,
+             const void* k, void* q_out, void* k_out, void* stream) {
+  return guarded([&] {
+    if (!prob) fail(MMI_ERR_INVALID_ARG, "problem is NULL");
+    mmi_problem p = *prob;
+    p.modality = nullptr;          // not read here, nor are the strides of v and o
+    p.v_stride_s = p.v_stride_h = p.o_stride_s = p.o_stride_h = 0;
+    const RopeArgs a = rope_args(normalise(&p), cfg, pos, q, k, q_out, k_out);
+    if (!ctx) fail(MMI_ERR_INVALID_ARG, "ctx is NULL");
+    OnDevice d(ctx->device);
+    HIPCHK(launch_rope(a, cfg->layout, (hipStream_t)stream));
+  });
+}
+
+int mmi_cache_write(mmi_ctx* ctx, const mmi_cache* cache, const void* k, int64_t k_stride_s, int64_t k_stride_h,
+                    const void* v, int64_t v_stride_s, int64_t v_stride_h, const int64_t* slot, int64_t n,
+                    void* stream) {
+  return guarded([&] {
+    const RowsArgs a = rows_args(cache, k, k_stride_s, k_stride_h, v, v_stride_s, v_stride_h, slot, n);
+    if (!ctx) fail(MMI_ERR_INVALID_ARG, "ctx is NULL");
+    OnDevice d(ctx->device);
+    HIPCHK(launch_cache_write(a, cache->type, (hipStream_t)stream));
+  });
+}
+
+int mmi_cache_read(mmi_ctx* ctx, const mmi_cache* cache, const int64_t* slot, int64_t n, void* k, int64_t k_stride_s,
+                   int64_t k_stride_h, void* v, int64_t v_stride_s, int64_t v_stride_h, void* stream) {
+  return guarded([&] {
+    const RowsArgs a = rows_args(cache, k, k_stride_s, k_stride_h, v, v_stride_s, v_stride_h, slot, n);
+    if (!ctx) fail(MMI_ERR_INVALID_ARG, "ctx is NULL");
+    OnDevice d(ctx->device);
+    HIPCHK(launch_cache_read(a, cache->type, (hipStream_t)stream));
+  });
+}
+
+int mmi_tree_workspace(mmi_ctx* ctx, const mmi_cache* cache, const mmi_tree* tree, size_t* bytes) {
+  return guarded([&] {
+    cache_dev(cache);
+    const mmi_tree t = tree_checked(cache, tree);
+    if (!ctx || !bytes) fail(MMI_ERR_INVALID_ARG, "ctx/bytes is NULL");
+    *bytes = tree_shape(t, cache->Hkv, ctx->cus).bytes;
+  });
+}
+
+int mmi_tree_attention(mmi_ctx* ctx, const mmi_cache* cache, const mmi_tree* tree, const void* q, const void* k,
+                       const void* v, void* o, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  return guarded([&] {
+    cache_dev(cache);
+    const mmi_tree t = tree_checked(cache, tree);
+    TreeArgs a = tree_args(cache, t, q, k, v, o, lse);
+    if (!ctx) fail(MMI_ERR_INVALID_ARG, "ctx is NULL");
+    const TreeShape s = tree_shape(t, cache->Hkv, ctx->cus);
+    if (!workspace || (uintptr_t)workspace % 16) fail(MMI_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    if (workspace_bytes < s.bytes)
+      fail(MMI_ERR_INVALID_ARG, "workspace of %zu bytes, %zu needed", workspace_bytes, s.bytes);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    a.part_o = reinterpret_cast<float*>(ws + s.part_o);
+    a.part_ml = reinterpret_cast<float*>(ws + s.part_ml);
+    a.rec = reinterpret_cast<int32_t*>(ws + s.rec);
+    a.target = s.target;
+    a.items = s.items;
+    OnDevice d(ctx->device);
+    HIPCHK(launch_tree(a, cache->type, s.rows, (hipStream_t)stream));
   });
 }
 

@@ -250,6 +250,7 @@ class Ctx:
         h = ct.c_void_p()
         _check(lib().mmi_ctx_create(device, ct.byref(h)))
         self.h = h
+        self.device = device
         self.plans = weakref.WeakSet()
         _live_ctx.add(self)
 

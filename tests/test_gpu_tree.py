@@ -1,0 +1,293 @@
+"""Attention of drafted tokens over the paged cache on the GPU against the
+oracle in fp64."""
+import numpy as np
+import pytest
+import torch
+
+from serving import Batch, D, f64
+
+pytestmark = pytest.mark.gpu
+KINDS = ["bf16", "fp8", "int8", "fp4"]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2504_16083_amd import mmi
+    return mmi.Ctx(0)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("L", [0, 1, 15, 33, 129, 700])
+def test_one_token(ctx, kind, page, L):
+    b = Batch(kind, [L], [1], 7, 1, page, seed=L + page)
+    b.check(*b.run(ctx))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("Hq,Hkv", [(28, 4), (8, 8), (2, 1), (40, 1)])
+def test_ragged_batch(ctx, kind, Hq, Hkv):
+    """Sequences of different sizes, empty ones among them, and padding rows behind the last."""
+    b = Batch(kind, [200, 0, 65, 31, 0, 512], [3, 2, 0, 1, 0, 9], Hq, Hkv, 32, seed=2, mask="tree", behind=5)
+    o, lse = b.run(ctx)
+    b.check(o, lse)
+    assert (o[-5:] == 7).all() and (lse[:, -5:] == 7).all()
+
+
+@pytest.mark.parametrize("T", [1, 5, 9, 10, 18, 19, 37, 64, 65, 130, 256])
+@pytest.mark.parametrize("mask", [None, "tree"])
+def test_drafted_tokens(ctx, T, mask):
+    """From one row to many tiles of them, masks of one to four words."""
+    b = Batch("bf16" if T % 2 else "int8", [95], [T], 7, 1, 16, seed=T, mask=mask)
+    o, lse = b.run(ctx)
+    pick = {(0, i) for i in {0, 1, T // 3, T // 2, T - 2, T - 1} if i >= 0}
+    b.check(o, lse, rows=pick)
+
+
+def test_many_sequences(ctx):
+    """More sequences than a workgroup has threads: the work list spans several passes over them."""
+    rng = np.random.default_rng(0)
+    lens = [int(x) for x in rng.integers(0, 60, 600)]
+    lens[300] = 2500
+    drafts = [int(x) for x in rng.integers(0, 3, 600)]
+    drafts[300] = 2
+    b = Batch("fp8", lens, drafts, 4, 2, 16, seed=3)
+    o, lse = b.run(ctx)
+    b.check(o, lse, rows={(s, i) for s in [0, 1, 2, 3, 4, 5, 254, 255, 256, 257, 300, 511, 512, 598, 599] for i in (0, 1)})
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("T,g", [(1, 7), (6, 8), (16, 7), (40, 7)])
+def test_long_cache(ctx, kind, T, g):
+    """Many chunks: the partial results are joined."""
+    b = Batch(kind, [40000, 17], [T, 1], 2 * g, 2, 64, seed=T, mask="tree")
+    o, lse = b.run(ctx)
+    b.check(o, lse, rows={(0, 0), (0, T - 1), (0, T // 2), (1, 0)})
+
+
+def test_rows_that_see_nothing(ctx):
+    """No cached token and an empty mask row: o = 0, lse = -inf. A mask need not hold a row's own token."""
+    b = Batch("bf16", [0, 5], [6, 3], 4, 2, 16, mask=lambda s, i, j: i != 2 and j < i)
+    o, lse = b.run(ctx)
+    b.check(o, lse)
+    assert (o[0] == 0).all() and (lse[:, 0] == -np.inf).all() and (o[2] == 0).all()
+
+
+@pytest.mark.parametrize("where", ["K", "V"])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_not_finite_drafts(ctx, where, value):
+    """An infinity or a NaN in the K or V of a drafted token reaches the rows that see the token, and no other."""
+    b = Batch("fp8", [40], [40], 4, 2, 16, seed=4, mask="tree")
+    x = b.k if where == "K" else b.v
+    for j, d in ((3, 0), (17, 127), (33, 64), (39, 5)):
+        x[j, 0, d] = value
+    o, lse = b.run(ctx)
+    with np.errstate(all="ignore"):
+        want = [(i, bool(b.sees[0][i][[3, 17, 33, 39]].any())) for i in range(40)]
+        got = f64(o)
+        for i, hit in want:
+            assert np.isfinite(got[i, 2:]).all()                 # the other KV head
+            if not hit:
+                assert np.isfinite(got[i]).all(), i
+        if where == "V":
+            b.check(o, lse)
+        else:
+            b.check(o, lse, rows={(0, i) for i, hit in want if not hit})
+            for i, hit in want:
+                # an infinite or undefined score: softmax has no value, but where all such are -inf
+                if hit and np.isnan(value):
+                    assert np.isnan(got[i, :2]).all()
+
+
+def test_several_not_finite_values_of_one_channel(ctx):
+    b = Batch("bf16", [3], [8], 2, 1, 16, seed=6, mask=lambda s, i, j: j in ((1, 2), (1, 3), (2, 4), (1,), (2,), (3,), (5,), (5, 1))[i])
+    b.v[1, 0, 9] = float("inf")
+    b.v[2, 0, 9] = float("-inf")
+    b.v[3, 0, 9] = float("inf")
+    b.v[4, 0, 9] = float("nan")
+    o, lse = b.run(ctx)
+    got = f64(o)[:, 0, 9]
+    assert np.isnan(got[0]) and got[1] == np.inf and np.isnan(got[2]) and got[3] == np.inf
+    assert got[4] == -np.inf and got[5] == np.inf and np.isfinite(got[6]) and got[7] == np.inf
+    other = np.delete(np.arange(D), 9)
+    assert np.isfinite(f64(o)[:, :, other]).all()
+
+
+def test_memory_behind_the_last_token(ctx):
+    """What lies behind a sequence's last token in its page (NaN here) has no part."""
+    b = Batch("bf16", [37, 18], [2, 1], 4, 2, 16)
+    used = np.zeros(b.cache.n_pages * 16, bool)
+    for s in b.slots:
+        used[s] = True
+    free = torch.from_numpy(np.flatnonzero(~used)).cuda()
+    for t in (b.cache.k, b.cache.v):
+        t[free // 16, :, free % 16] = float("nan")
+    b.check(*b.run(ctx))
+
+
+def test_bad_pages_lengths_and_rows(ctx):
+    """Device arrays with values out of range: nothing is read or written out of place, as documented."""
+    b = Batch("int8", [100, 40, 64], [4, 4, 4], 4, 2, 16, seed=5, behind=2)
+    b.tree.pages[0, 2] = b.cache.n_pages                         # one page behind the pool: its tokens do not exist
+    b.tree.pages[0, 4] = -7
+    b.tree.pages[0, 5] = 2 ** 31 - 1
+    gone = np.ones(100, bool)
+    gone[32:48] = gone[64:96] = False
+    o, lse = b.run(ctx)
+    b.check(o, lse, visible=lambda s: gone if s == 0 else np.ones(b.lens[s], bool))
+    good = o.clone(), lse.clone()
+    # lengths are cut to [0, max_len]
+    b.tree.length.copy_(torch.tensor([10 ** 9, 40, -5], dtype=torch.int32))
+    o, lse = b.run(ctx)
+    assert torch.equal(o[:8], good[0][:8]) and torch.equal(lse[:, :8], good[1][:, :8])
+    b.lens[2], b.slots[2] = 0, b.slots[2][:0]
+    b.check(o, lse, rows={(2, i) for i in range(4)})
+    # rows beyond max_rows and beyond the tensors are left alone
+    b.tree.length.copy_(torch.tensor([100, 40, 0], dtype=torch.int32))
+    b.tree.row_start.copy_(torch.tensor([-3, 4, 9, 10 ** 6], dtype=torch.int32))
+    o, lse = b.run(ctx)
+    assert torch.equal(o[:4], good[0][:4]) and (o[8] == 7).all() and (o[13] == 7).all()
+    assert (o[9:13] != 7).any()
+
+
+def test_scores_of_any_size(ctx):
+    """A large scale, and scores that leave single keys: the running maximum moves far."""
+    b = Batch("bf16", [900], [3], 4, 1, 64, seed=8)
+    b.tree.scale = b.scale = 3.0
+    b.check(*b.run(ctx))
+    b = Batch("bf16", [300], [2], 2, 1, 64, seed=9)
+    b.q.mul_(0)
+    o, lse = b.run(ctx)
+    b.check(o, lse)
+
+
+def test_strides(ctx):
+    """q, k, v as views of a fused projection, o as a view of a wider buffer, pages among those of other layers."""
+    from paper_2504_16083_amd import cache as KV
+    b = Batch("fp8", [70, 200], [5, 3], 6, 2, 32, seed=10, mask="tree", words=3)
+    want, lse = b.run(ctx)
+    fused = torch.zeros(b.n, 14, D, dtype=torch.bfloat16, device="cuda")
+    fused[:, 1:7], fused[:, 8:10], fused[:, 12:14] = b.q, b.k, b.v
+    wide = torch.full((b.n, 9, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    c = b.cache
+    mem = torch.zeros(c.n_pages, 3, 2, 2, 32, 128, dtype=torch.uint8, device="cuda")
+    sc = torch.zeros(c.n_pages, 3, 2, 2, 32, 4, dtype=torch.uint8, device="cuda")
+    mem[:, 1, 0], mem[:, 1, 1], sc[:, 1, 0], sc[:, 1, 1] = c.k, c.v, c.k_scale, c.v_scale
+    c = KV.Cache("fp8", mem[:, 1, 0], mem[:, 1, 1], sc[:, 1, 0], sc[:, 1, 1])
+    KV.mmi_tree_attention(ctx, c, b.tree, fused[:, 1:7], fused[:, 8:10], fused[:, 12:14], wide[:, 2:8], b.workspace(ctx))
+    assert torch.equal(wide[:, 2:8], want) and (wide[:, :2] == 7).all() and (wide[:, 8:] == 7).all()
+
+
+def test_workspace_bounds(ctx):
+    from paper_2504_16083_amd import cache as KV, mmi
+    b = Batch("bf16", [500], [2], 4, 2, 64)
+    ws = b.workspace(ctx)
+    o, _ = b.outputs()
+    with pytest.raises(mmi.MMIError, match="workspace"):
+        KV.mmi_tree_attention(ctx, b.cache, b.tree, b.q, b.k, b.v, o, ws[:-256])
+    # no byte outside it is touched, and what it held does not matter
+    big = torch.full((ws.numel() + 8192,), 0xff, dtype=torch.uint8, device="cuda")
+    KV.mmi_tree_attention(ctx, b.cache, b.tree, b.q, b.k, b.v, o, big[4096:-4096])
+    assert (big[:4096] == 0xff).all() and (big[-4096:] == 0xff).all()
+    b.check(o)
+    big = KV.Tree(torch.zeros(4097, dtype=torch.int32, device="cuda"), torch.zeros(4096, dtype=torch.int32, device="cuda"),
+                  torch.zeros(4096, 1, dtype=torch.int32, device="cuda"), max_rows=256, max_len=10)
+    with pytest.raises(mmi.MMIError, match="workgroups"):
+        KV.mmi_tree_workspace(ctx, b.cache, big, 1024, 1 << 20)
+
+
+def test_no_rows(ctx):
+    b = Batch("bf16", [], [], 4, 2, 64)
+    b.run(ctx)
+    b = Batch("bf16", [30], [0], 4, 2, 64, behind=3)
+    o, lse = b.run(ctx)
+    assert (o == 7).all() and (lse == 7).all()
+
+
+def test_streams_and_graphs(ctx):
+    """Two batches at once on streams of their own (a workspace each), and a captured call replayed with other
+    lengths, rows and pages within its bounds."""
+    from paper_2504_16083_amd import cache as KV
+    a, b = Batch("fp8", [3000, 900], [4, 2], 14, 2, 64, seed=1), Batch("int8", [5000], [6], 14, 2, 64, seed=2, mask="tree")
+    want = a.run(ctx)[0], b.run(ctx)[0]
+    streams, outs, spaces = [torch.cuda.Stream() for _ in "ab"], [x.outputs()[0] for x in (a, b)], [x.workspace(ctx) for x in (a, b)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for x, st, o, ws in zip((a, b), streams, outs, spaces):
+            KV.mmi_tree_attention(ctx, x.cache, x.tree, x.q, x.k, x.v, o, ws, stream=st)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+    graph, o = torch.cuda.CUDAGraph(), torch.zeros_like(outs[0])
+    with torch.cuda.graph(graph):
+        KV.mmi_tree_attention(ctx, a.cache, a.tree, a.q, a.k, a.v, o, spaces[0])
+    for lens, start in (([3000, 900], [0, 4, 6]), ([17, 0], [0, 1, 2]), ([0, 3000 - 2100], [0, 3, 6]), ([2999, 64], [0, 0, 4])):
+        a.tree.length.copy_(torch.tensor(lens, dtype=torch.int32))
+        a.tree.row_start.copy_(torch.tensor(start, dtype=torch.int32))
+        o.fill_(7.0)
+        graph.replay()
+        eager = a.run(ctx)[0]
+        torch.cuda.synchronize()
+        assert torch.equal(o, eager)
+
+
+def test_results_repeat(ctx):
+    b = Batch("fp4", [9000, 100, 2500], [7, 1, 12], 14, 2, 16, seed=11, mask="tree")
+    first = b.run(ctx)
+    for _ in range(3):
+        again = b.run(ctx)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_offsets_past_32_bits(ctx):
+    """Pages whose place in memory lies beyond 2^32 bytes."""
+    from paper_2504_16083_amd import cache as KV
+    b = Batch("bf16", [600], [2], 4, 2, 256, seed=12)
+    want = b.run(ctx)[0]
+    n = b.cache.n_pages
+    k, v = (torch.empty(40000, 2, 256, D, dtype=torch.bfloat16, device="cuda") for _ in "kv")     # 5.2 GB each
+    k[-n:], v[-n:] = b.cache.k, b.cache.v
+    pages = torch.where(b.tree.pages >= 0, b.tree.pages + len(k) - n, -1)
+    tree = KV.Tree(b.tree.row_start, b.tree.length, pages, max_rows=b.max_rows, max_len=b.max_len)
+    o, _ = b.outputs()
+    cache = KV.Cache("bf16", k, v)
+    KV.mmi_tree_attention(ctx, cache, tree, b.q, b.k, b.v, o, b.workspace(ctx))
+    assert torch.equal(o, want)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_prefill_then_decode(ctx, kind):
+    """The operators as they are used: positions on Q and K, the prefill's keys and values into the cache, and the
+    last tokens attended over it as a chain of drafts, against the library's dense prefill of the whole."""
+    from paper_2504_16083_amd import cache as KV, mmi
+    S, T, Hq, Hkv, page = 1500, 11, 14, 2, 64
+    g = torch.Generator().manual_seed(0)
+    fused = torch.randn(S, Hq + 2 * Hkv, D, generator=g).to(torch.bfloat16).cuda()
+    q, k, v = fused[:, :Hq], fused[:, Hq:Hq + Hkv], fused[:, Hq + Hkv:]
+    KV.mmi_rope(ctx, KV.RopeCfg(theta=1e6, scaling="parts", factor=4.0, orig_len=512), q, k)
+    n = S - T
+    cache = KV.Cache.empty(kind, 30, Hkv, page)
+    pages = torch.randperm(30, generator=g)[:-(-n // page)].to(torch.int32).cuda()
+    i = torch.arange(n, device="cuda")
+    slot = pages.long()[i // page] * page + i % page
+    KV.mmi_cache_write(ctx, cache, k[:n], v[:n], slot)
+    kk, vv = k.contiguous().clone(), v.contiguous().clone()
+    KV.mmi_cache_read(ctx, cache, slot, kk[:n], vv[:n])          # what decoding will see of the prompt
+    want, lse = torch.empty(S, Hq, D, dtype=torch.bfloat16, device="cuda"), torch.empty(Hq, S, device="cuda")
+    mmi.mmi_dense_attention(ctx, mmi.Problem(S, Hq, Hkv), q.contiguous(), kk, vv, want, lse)
+    tree = KV.Tree(torch.tensor([0, T], dtype=torch.int32, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda"),
+                   pages[None], max_rows=T, max_len=n)
+    o, l = torch.empty(T, Hq, D, dtype=torch.bfloat16, device="cuda"), torch.empty(Hq, T, device="cuda")
+    ws = torch.empty(KV.mmi_tree_workspace(ctx, cache, tree, Hq, T), dtype=torch.uint8, device="cuda")
+    KV.mmi_tree_attention(ctx, cache, tree, q[n:], k[n:], v[n:], o, ws, lse=l)
+    # both are within the weights' rounding (half a step of the mean |v|, at most 4 here) and half a step of
+    # the result of the exact value
+    a, b = f64(o), f64(want[n:])
+    assert (np.abs(a - b) <= 2 * 2.0 ** -8 * (4.0 + np.abs(b))).all()
+    assert torch.allclose(l, lse[:, n:], atol=1e-3)
+    assert np.linalg.norm(a - b) <= 2.0 ** -7 * np.linalg.norm(b)
+    # the accepted drafts follow into the cache, the others do not
+    keep = torch.tensor([n + j if j % 2 == 0 else -1 for j in range(T)], device="cuda")
+    before = cache.k.clone()
+    place = torch.where(keep >= 0, pages.long()[torch.clamp(keep, 0, len(pages) * page - 1) // page] * page + keep % page, -1)
+    KV.mmi_cache_write(ctx, cache, k[n:], v[n:], place)
+    assert int((cache.k != before).flatten(3).any(-1).any(1).sum()) == sum(1 for j in range(0, T, 2))

@@ -1,0 +1,165 @@
+"""include/mmi_cache.h without a device: the library exports what the header
+declares, the structures agree, and bad arguments are refused with the
+documented codes before anything is launched."""
+import ctypes as ct
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2504_16083_amd import cache as KV
+from paper_2504_16083_amd import mmi
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+DEV = 1 << 20                    # an address; no call here comes as far as using it
+INVALID, UNSUPPORTED, BAD_CONFIG = -1, -2, -3
+
+
+def test_symbols_and_structures():
+    src = open(os.path.join(ROOT, "include", "mmi_cache.h")).read()
+    names = set(re.findall(r"^int\s+(mmi_\w+)\s*\(", src, re.M))
+    assert names == set(KV.SYMBOLS)
+    L = KV.lib()
+    assert all(hasattr(L, n) for n in names)
+    assert KV.mmi_rope_cfg.theta.offset == 32 and ct.sizeof(KV.mmi_rope_cfg) == 88
+    assert KV.mmi_cache.page_stride.offset == 56 and ct.sizeof(KV.mmi_cache) == 72
+    assert KV.mmi_tree.scale.offset == 128 and ct.sizeof(KV.mmi_tree) == 136
+
+
+def rope(prob=None, cfg=None, q=DEV, k=DEV, qo=DEV, ko=DEV, pos=None, **kw):
+    c = KV.mmi_rope_cfg(128, 0, 0, 0, (ct.c_int32 * 3)(0, 0, 0), 0, 10000.0, 1.0, 0.0, 32.0, 1.0, 0.0, None)
+    for name, value in kw.items():
+        setattr(c, name, value)
+    p = prob or mmi.Problem(100, 4, 2)
+    return KV.lib().mmi_rope(None, ct.byref(p.c), None if cfg == 0 else ct.byref(c), pos, q, k, qo, ko, None)
+
+
+def test_rope_refusals():
+    assert rope() == INVALID and "ctx" in mmi.mmi_last_error()       # all but the context is right
+    assert KV.lib().mmi_rope(None, None, None, None, None, None, None, None, None) == INVALID
+    assert rope(cfg=0) == INVALID
+    for r in (0, 8, 24, 144, -16):
+        assert rope(rot_dim=r) == UNSUPPORTED
+    for kw in ({"layout": 2}, {"scaling": 4}, {"scaling": -1}, {"inverse": 2}, {"theta": 0.0}, {"theta": float("nan")},
+               {"scaling": 1, "factor": 0.5}, {"scaling": 3, "factor": 2.0, "orig_len": 0.0},
+               {"scaling": 3, "factor": 2.0, "orig_len": 10.0, "beta_fast": 1.0}, {"attn_factor": -1.0},
+               {"sections": (ct.c_int32 * 3)(16, 24, 25)}, {"sections": (ct.c_int32 * 3)(-1, 40, 25)}):
+        assert rope(**kw) == BAD_CONFIG, kw
+    assert rope(reserved=1) == INVALID
+    table = (ct.c_double * 64)(*([1.0] * 63 + [float("inf")]))
+    assert rope(inv_freq=table) == BAD_CONFIG
+    table[63] = -1.0
+    assert rope(inv_freq=table) == BAD_CONFIG
+    table[63] = 100.0
+    assert rope(inv_freq=table, theta=0.0) == INVALID and "ctx" in mmi.mmi_last_error()
+    assert rope(q=None, qo=None) == INVALID and "ctx" in mmi.mmi_last_error()
+    assert rope(q=None, qo=None, k=None, ko=None) == INVALID and "NULL" in mmi.mmi_last_error()
+    assert rope(q=None) == INVALID and rope(ko=None) == INVALID
+    assert rope(q=DEV + 8) == INVALID and rope(ko=DEV + 2) == INVALID and rope(pos=DEV + 2) == INVALID
+    assert rope(mmi.Problem(0, 4, 2)) == INVALID and rope(mmi.Problem(100, 3, 2)) == UNSUPPORTED
+    assert rope(mmi.Problem(100, 4, 2, strides={"q": (516, 128)})) == INVALID
+    assert rope(mmi.Problem(100, 4, 2, strides={"q": (0, 128)})) == INVALID
+
+
+def pool(**kw):
+    c = KV.mmi_cache(1, 64, 2, 128, 10, DEV, DEV, DEV, DEV, 0, 0)
+    for name, value in kw.items():
+        setattr(c, name, value)
+    return c
+
+
+def rows(c, n=5, k=DEV, v=DEV, slot=DEV, ks=(0, 0), vs=(0, 0)):
+    p = None if c is None else ct.byref(c)
+    a = KV.lib().mmi_cache_write(None, p, k, *ks, v, *vs, slot, n, None)
+    assert a == KV.lib().mmi_cache_read(None, p, slot, n, k, *ks, v, *vs, None)
+    return a
+
+
+def test_cache_refusals():
+    assert rows(pool()) == INVALID and "ctx" in mmi.mmi_last_error()
+    assert rows(None) == INVALID
+    assert rows(pool(type=4)) == BAD_CONFIG and rows(pool(type=-1)) == BAD_CONFIG
+    assert rows(pool(D=64)) == UNSUPPORTED
+    for page in (0, 8, 48, 512, -16):
+        assert rows(pool(page=page)) == UNSUPPORTED
+    assert rows(pool(Hkv=0)) == INVALID and rows(pool(Hkv=2000)) == UNSUPPORTED
+    assert rows(pool(n_pages=0)) == INVALID and rows(pool(n_pages=1 << 31)) == UNSUPPORTED
+    assert rows(pool(k=None)) == INVALID and rows(pool(v=DEV + 8)) == INVALID
+    assert rows(pool(k_scale=None)) == INVALID and rows(pool(v_scale=DEV + 2)) == INVALID
+    assert rows(pool(type=0, k_scale=None, v_scale=None)) == INVALID and "ctx" in mmi.mmi_last_error()
+    packed = 64 * 2 * 128
+    assert rows(pool(page_stride=packed - 16)) == INVALID and rows(pool(page_stride=packed + 8)) == INVALID
+    assert rows(pool(scale_stride=64 * 2 * 4 - 4)) == INVALID and rows(pool(scale_stride=64 * 2 * 4 + 2)) == INVALID
+    assert rows(pool(page_stride=packed + 16, scale_stride=64 * 2 * 4 + 4)) == INVALID
+    assert "ctx" in mmi.mmi_last_error()
+    assert rows(pool(page_stride=1 << 41)) == UNSUPPORTED
+    assert rows(pool(), n=-1) == INVALID and rows(pool(), n=(1 << 25) + 1) == UNSUPPORTED
+    assert rows(pool(), k=None) == INVALID and rows(pool(), v=DEV + 4) == INVALID and rows(pool(), slot=DEV + 4) == INVALID
+    assert rows(pool(), ks=(252, 128)) == INVALID and rows(pool(), vs=(-256, 128)) == INVALID
+    assert rows(pool(), n=0, k=None, v=None, slot=None) == INVALID and "ctx" in mmi.mmi_last_error()
+
+
+def tree(c=None, q=DEV, o=DEV, ws=DEV, bytes=1 << 40, lse=None, **kw):
+    t = KV.mmi_tree(n_seq=3, n_rows=9, Hq=8, max_rows=3, max_len=100, max_pages=2, mask_words=1, row_start=DEV,
+                    length=DEV, pages=DEV, mask=DEV)
+    for name, value in kw.items():
+        setattr(t, name, value)
+    c = c or pool()
+    need = ct.c_size_t()
+    L = KV.lib()
+    a = L.mmi_tree_attention(None, ct.byref(c), ct.byref(t), q, DEV, DEV, o, lse, ws, bytes, None)
+    b = L.mmi_tree_workspace(None, ct.byref(c), ct.byref(t), ct.byref(need))
+    return a, b
+
+
+def test_tree_refusals():
+    both = lambda code: (code, code)  # noqa: E731
+    assert tree() == both(INVALID) and "ctx" in mmi.mmi_last_error()
+    assert KV.lib().mmi_tree_attention(None, ct.byref(pool()), None, DEV, DEV, DEV, DEV, None, DEV, 1, None) == INVALID
+    assert KV.lib().mmi_tree_workspace(None, None, None, None) == INVALID
+    for kw in ({"n_seq": -1}, {"n_rows": -1}, {"Hq": 0}, {"max_rows": 0}, {"max_len": -1}, {"max_pages": 1},
+               {"max_pages": -1}, {"mask_words": 0}, {"max_rows": 65}, {"scale": -1.0}, {"scale": float("nan")},
+               {"reserved": 1}, {"q_stride_s": 12, "q_stride_h": 128}, {"o_stride_s": 1024}):
+        assert tree(**kw) == both(INVALID), kw
+    for kw in ({"n_seq": 5000}, {"n_rows": (1 << 20) + 1}, {"Hq": 7}, {"Hq": 2048}, {"max_rows": 257},
+               {"max_len": (1 << 30) + 1, "max_pages": 1 << 25}, {"k_stride_s": 1 << 41, "k_stride_h": 128}):
+        assert tree(**kw) == both(UNSUPPORTED), kw
+    assert tree(pool(type=9)) == both(BAD_CONFIG)
+    # only the attention call takes these
+    for kw in ({"q": None}, {"o": DEV + 8}, {"lse": DEV + 2}, {"row_start": None}, {"length": DEV + 1}, {"pages": None},
+               {"mask": DEV + 4}):
+        assert tree(**kw)[0] == INVALID, kw
+        assert KV.lib().mmi_tree_workspace is not None
+    assert tree(pages=None, max_len=0)[0] == INVALID and "ctx" in mmi.mmi_last_error()
+
+
+class _Ctx:
+    device, h = 0, None
+
+
+def test_binding_refusals():
+    """What the C side cannot see: types, shapes and devices of the tensors."""
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    with pytest.raises(ValueError, match="bfloat16"):
+        KV.mmi_rope(_Ctx, KV.RopeCfg(), q=torch.zeros(4, 2, 128))
+    with pytest.raises(ValueError, match="context"):
+        KV.mmi_rope(_Ctx, KV.RopeCfg(), q=bf(4, 2, 128))
+    with pytest.raises(ValueError, match="neither"):
+        KV.mmi_rope(_Ctx, KV.RopeCfg())
+    with pytest.raises(ValueError):
+        KV.RopeCfg(layout="other")
+    with pytest.raises(ValueError):
+        KV.RopeCfg(rot_dim=64, inv_freq=[1.0] * 31)
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)  # noqa: E731
+    with pytest.raises(ValueError, match="scales"):
+        KV.Cache("fp8", u8(3, 2, 16, 128), u8(3, 2, 16, 128))
+    with pytest.raises(ValueError, match="shape"):
+        KV.Cache("fp4", u8(3, 2, 16, 128), u8(3, 2, 16, 128), u8(3, 2, 16, 4), u8(3, 2, 16, 4))
+    with pytest.raises(ValueError, match="contiguous"):
+        KV.Cache("bf16", bf(3, 16, 2, 128).transpose(1, 2), bf(3, 16, 2, 128).transpose(1, 2))
+    with pytest.raises(ValueError, match="unknown"):
+        KV.Cache("fp16", bf(3, 2, 16, 128), bf(3, 2, 16, 128))
+    c = KV.Cache("bf16", bf(3, 2, 16, 128), bf(3, 2, 16, 128))
+    with pytest.raises(ValueError, match="context"):
+        KV.mmi_cache_write(_Ctx, c, bf(4, 2, 128), bf(4, 2, 128), torch.zeros(4, dtype=torch.int64))
