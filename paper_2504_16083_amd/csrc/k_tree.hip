@@ -483,6 +483,438 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   }
 }
 
+// ------------------------------------------------------------------ many rows
+// With more than 64 rows a head the products, not the cache's bytes, bound the
+// work, and a staged key has to serve as many rows as registers hold: a wave
+// has two tiles of 32 rows (512 registers, one wave a SIMD), so that every K
+// and V operand read from LDS feeds two MFMAs. The workgroup's four waves are
+// WR groups of rows times 4 / WR groups of keys; keys go through three LDS
+// stages of 64, one barrier a stage.
+//
+// A unit is 32 keys x 32 rows (one tile); a wave's units alternate its tiles.
+// Slot u issues QK of unit u + 1 and PV of unit u - 1 (8 MFMAs each, in turn)
+// with the softmax of unit u spread between them, since the vector ALU
+// overlaps only MFMAs of the same wave. Even slots (tile 0) use the operands
+// of a key block for the last time and read those of the next one into the
+// same registers behind each MFMA.
+constexpr int SK = 64;                 // keys of a stage
+constexpr int NST = 3;
+
+struct __align__(16) Stage64 {
+  uint16_t k[SK * TK];
+  uint16_t v[SK * TV];
+};
+
+template <int TYPE>
+struct Raw64 {                         // a thread's pieces of a stage: keys key0 + i * RP
+  static constexpr int CPR = Codec<TYPE>::ROW / 16, RP = 256 / CPR, N = SK / RP;
+  u32x4 k[N], v[N];
+  uint32_t ks[N], vs[N];
+  int ok[N];
+};
+
+struct KeySource {
+  const int32_t* pages;
+  int head, c1, tid;
+};
+
+template <int TYPE>
+__device__ __forceinline__ void page_ids(int (&p)[Raw64<TYPE>::N], const TreeArgs& a, const KeySource& s, int t0) {
+#pragma unroll
+  for (int i = 0; i < Raw64<TYPE>::N; ++i) {
+    const int t = t0 + s.tid / Raw64<TYPE>::CPR + i * Raw64<TYPE>::RP;
+    p[i] = s.pages[min(t, s.c1 - 1) >> a.c.shift];
+  }
+}
+
+template <int TYPE>
+__device__ __forceinline__ void load_stage(Raw64<TYPE>& r, const int (&p)[Raw64<TYPE>::N], const TreeArgs& a,
+                                           const KeySource& s, int t0) {
+  typedef Raw64<TYPE> R;
+#pragma unroll
+  for (int i = 0; i < R::N; ++i) {
+    const int t = t0 + s.tid / R::CPR + i * R::RP;
+    const bool there = (uint32_t)p[i] < (uint64_t)a.c.n_pages;
+    r.ok[i] = there && t < s.c1;
+    const int64_t page = there ? p[i] : 0;
+    const int in = (s.head << a.c.shift) + (t & ((1 << a.c.shift) - 1));
+    const int64_t at = page * a.c.page_stride + (int64_t)in * Codec<TYPE>::ROW + s.tid % R::CPR * 16;
+    r.k[i] = *reinterpret_cast<const u32x4*>(a.c.k + at);
+    r.v[i] = *reinterpret_cast<const u32x4*>(a.c.v + at);
+    if constexpr (Codec<TYPE>::SCALED) {
+      const int64_t sat = page * a.c.scale_stride + (int64_t)in * 4;
+      r.ks[i] = *reinterpret_cast<const uint32_t*>((const uint8_t*)a.c.ks + sat);
+      r.vs[i] = *reinterpret_cast<const uint32_t*>((const uint8_t*)a.c.vs + sat);
+    }
+  }
+}
+
+template <int TYPE>
+__device__ __forceinline__ void write_stage(Stage64& st, const Raw64<TYPE>& r, int tid) {
+  typedef Raw64<TYPE> R;
+#pragma unroll
+  for (int i = 0; i < R::N; ++i) {
+    const int key = tid / R::CPR + i * R::RP, piece = tid % R::CPR;
+    const u32x4 none = {};
+    put_piece<TYPE>(&st.k[key * TK], r.k[i], r.ks[i], piece);
+    put_piece<TYPE>(&st.v[key * TV], r.ok[i] ? r.v[i] : none, r.ok[i] ? r.vs[i] : 0u, piece);
+  }
+}
+
+struct Tiles {                         // a wave's 64 rows
+  f32x16 o[2][4];
+  bf16x8 q[2][8];
+  float m[2], l[2], lo[2];
+};
+
+__device__ __forceinline__ bf16x8 k_read(const Stage64& st, int sub, int x, int c, int h) {
+  return *reinterpret_cast<const bf16x8*>(&st.k[(32 * sub + c) * TK + h * 64 + x * 8]);
+}
+
+__device__ __forceinline__ bf16x8 v_read(const Stage64& st, int sub, int x, int vlane) {   // x: half, dt
+  const uint16_t* p = &st.v[vlane + (32 * sub + 16 * (x >> 2)) * TV + 32 * (x & 3)];
+  const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p));
+  const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p + 8 * TV));
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+__device__ __forceinline__ void mask_unit(f32x16& s, uint32_t seen, int h) {
+  const uint32_t mine = seen >> (4 * h);
+#pragma unroll
+  for (int x = 0; x < 16; ++x)
+    if (!(mine >> (8 * (x >> 2) + (x & 3)) & 1)) s[x] = -INFINITY;
+}
+
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16e2;
+
+// The softmax of a unit in pieces that fit between MFMAs: 0, 1 maxima of 8
+// scores, 2 the running maximum, 3-18 one exponential each, 19, 20 packing
+// and the sum of the packed, 21 the sums.
+constexpr int PIECES = 22;
+struct SoftState {
+  float mx, base, alpha, rs, ro;
+};
+
+__device__ __forceinline__ void soft_piece(int piece, f32x16& s, float sc, float& m, float& l, float& lo,
+                                           bf16x8 (&p)[2], SoftState& z) {
+  if (piece < 2) {
+    float mx = s[8 * piece];
+#pragma unroll
+    for (int x = 1; x < 8; ++x) mx = fmaxf(mx, s[8 * piece + x]);
+    z.mx = piece == 0 ? mx : fmaxf(z.mx, mx);
+  } else if (piece == 2) {
+    const float mx = half_max(z.mx) * sc;
+    const bool move = __any(mx > m + SLACK);
+    const float mn = move ? fmaxf(m, mx) : m;
+    z.alpha = m == mn ? 1.0f : fast_exp2(m - mn);
+    m = mn;
+    z.base = mn == -INFINITY ? 0.0f : mn;
+    z.rs = z.ro = 0.0f;
+  } else if (piece < 19) {
+    const int x = piece - 3;
+    s[x] = fast_exp2(fmaf(s[x], sc, -z.base));
+    z.rs += s[x];
+  } else if (piece < 21) {
+    const int half = piece - 19;
+    const bf16e2 one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+    for (int x = 0; x < 8; ++x) p[half][x] = (__bf16)s[8 * half + x];
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      z.ro = __builtin_amdgcn_fdot2_f32_bf16(bf16e2{p[half][2 * x], p[half][2 * x + 1]}, one, z.ro, false);
+  } else {
+    l = l * z.alpha + half_sum(z.rs);
+    lo = lo * z.alpha + half_sum(z.ro);
+  }
+}
+
+// One slot: softmax of tile X's unit (scores s_sm), QK of the other tile's
+// next unit into s_qk, PV of the other tile's last unit. READ (even slots):
+// the K of the next key block and the V of this one follow their registers'
+// last use.
+template <int X, bool READ>
+__device__ __forceinline__ void slot(Tiles& w, bf16x8 (&kr)[8], bf16x8 (&vr)[8], f32x16& s_sm, f32x16& s_qk,
+                                     const bf16x8 (&p_pv)[2], bf16x8 (&p_sm)[2], float sc, const Stage64& knext,
+                                     int ksub, const Stage64& vnext, int vsub, int c, int h, int vlane) {
+  constexpr int Y = 1 - X;
+  SoftState z;
+  int pc = 0;
+  const f32x16 zero = {};
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int x = i >> 1;
+    if ((i & 1) == 0) {
+      s_qk = mfma32(kr[x], w.q[Y][x], x == 0 ? zero : s_qk);
+      if (READ) kr[x] = k_read(knext, ksub, x, c, h);
+    } else {
+      w.o[Y][x & 3] = mfma32(vr[x], p_pv[x >> 2], w.o[Y][x & 3]);
+      if (READ) vr[x] = v_read(vnext, vsub, x, vlane);
+    }
+    const int end = (i + 1) * PIECES / 16;
+#pragma unroll
+    for (; pc < end; ++pc) soft_piece(pc, s_sm, sc, w.m[X], w.l[X], w.lo[X], p_sm, z);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (__any(z.alpha != 1.0f)) {
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) w.o[X][dt][x] *= z.alpha;
+  }
+}
+
+// A staged block of 32 keys against one tile, nothing overlapped.
+__device__ __forceinline__ void unit_alone(Tiles& w, int X, const Stage64& st, int sub, uint32_t seen, float sc,
+                                           int c, int h, int vlane) {
+  f32x16 s = {};
+#pragma unroll
+  for (int x = 0; x < 8; ++x) s = mfma32(k_read(st, sub, x, c, h), w.q[X][x], s);
+  mask_unit(s, seen, h);
+  SoftState z;
+  bf16x8 p[2];
+#pragma unroll
+  for (int pc = 0; pc < PIECES; ++pc) soft_piece(pc, s, sc, w.m[X], w.l[X], w.lo[X], p, z);
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) w.o[X][dt][x] *= z.alpha;
+#pragma unroll
+  for (int x = 0; x < 8; ++x) w.o[X][x & 3] = mfma32(v_read(st, sub, x, vlane), p[x >> 2], w.o[X][x & 3]);
+}
+
+template <int TYPE, int WR>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_tree_wide(TreeArgs a) {
+  constexpr int ROWS = 64 * WR, WK = 4 / WR, SUBS = 2 / WK;   // rows a workgroup, key groups, a wave's blocks a stage
+  __shared__ Stage64 st[NST];
+  __shared__ int64_t sh64[4];
+  __shared__ int sh[8];
+  Item it;
+  if (!find_item<ROWS>(a, blockIdx.x, it, sh64, sh)) return;
+  const Seq sq = sequence(a, it.b);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int wr = wave % WR, wk = wave / WR;
+  const int c = lane & 31, h = lane >> 5;
+  const int grp = lane >> 4, li = lane & 15;
+  const int vlane = (4 * (grp >> 1) + (li >> 2)) * TV + 16 * (grp & 1) + 4 * (li & 3);
+  const int row0 = it.tile * ROWS + 64 * wr;               // the wave's first row
+  const bool active = row0 < sq.T * a.g;
+
+  Tiles w;
+  int tok[2];
+#pragma unroll
+  for (int X = 0; X < 2; ++X) {
+    const int row = row0 + 32 * X + c;
+    tok[X] = row / a.g;
+    const bool live = tok[X] < sq.T;
+    const uint16_t* q = (const uint16_t*)a.q.p + (int64_t)(sq.row0 + (live ? tok[X] : 0)) * a.q.ss +
+                        (int64_t)(it.head * a.g + (live ? row - tok[X] * a.g : 0)) * a.q.sh + h * 64;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const bf16x8 y = load16(q + 8 * x);
+      w.q[X][x] = live ? y : zero8();
+    }
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) w.o[X][dt][x] = 0.0f;
+    w.m[X] = -INFINITY;
+    w.l[X] = w.lo[X] = 0.0f;
+  }
+
+  const int steps = (it.c1 - it.c0 + SK - 1) / SK;
+  if (steps > 0) {
+    const KeySource src = {a.pages + (int64_t)it.b * a.max_pages, it.head, it.c1, tid};
+    // pages outside the cache are rare enough to ask once for the whole chunk
+    int bad = 0;
+    for (int p = (it.c0 >> a.c.shift) + tid; p <= (it.c1 - 1) >> a.c.shift; p += 256)
+      bad |= (uint32_t)src.pages[p] >= (uint64_t)a.c.n_pages;
+    const bool any_bad = __syncthreads_or(bad);
+    auto seen_of = [&](int t0) -> uint32_t {               // keys of a block of 32 that exist
+      uint32_t m = it.c1 - t0 >= 32 ? 0xffffffffu : it.c1 <= t0 ? 0u : (1u << (it.c1 - t0)) - 1;
+      if (any_bad)
+        for (int half = 0; half < 2; ++half) {
+          const int t = min(t0 + 16 * half, it.c1 - 1);
+          if ((uint32_t)src.pages[t >> a.c.shift] >= (uint64_t)a.c.n_pages) m &= half ? 0x0000ffffu : 0xffff0000u;
+        }
+      return m;
+    };
+    Raw64<TYPE> raw;
+    int pid[Raw64<TYPE>::N];
+    page_ids<TYPE>(pid, a, src, it.c0);
+    load_stage<TYPE>(raw, pid, a, src, it.c0);
+    page_ids<TYPE>(pid, a, src, it.c0 + SK);
+    write_stage<TYPE>(st[0], raw, tid);
+    load_stage<TYPE>(raw, pid, a, src, it.c0 + SK);
+    page_ids<TYPE>(pid, a, src, it.c0 + 2 * SK);
+    __syncthreads();
+    bf16x8 kr[8], vr[8], p0[2], p1[2];
+    f32x16 s0 = {}, s1 = {};
+    const int first = WK == 1 ? 0 : wk;                    // the wave's first block of a stage
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      kr[x] = k_read(st[0], first, x, c, h);
+      vr[x] = zero8();
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) p0[x] = p1[x] = zero8();
+#pragma unroll
+    for (int x = 0; x < 8; ++x) s0 = mfma32(kr[x], w.q[0][x], s0);
+    write_stage<TYPE>(st[1], raw, tid);
+    if (steps > 2) load_stage<TYPE>(raw, pid, a, src, it.c0 + 2 * SK);
+    if (steps > 3) page_ids<TYPE>(pid, a, src, it.c0 + 3 * SK);
+    int cur = 0;
+    for (int t = 0; t < steps; ++t) {
+      const int nxt = cur == NST - 1 ? 0 : cur + 1, far = nxt == NST - 1 ? 0 : nxt + 1;
+#pragma unroll
+      for (int j = 0; j < SUBS; ++j) {
+        const int sub = WK == 1 ? j : wk;
+        const bool last = j == SUBS - 1;
+        // stage t + 1 is whole, and everybody is through with stage t - 1
+        if (last) __syncthreads();
+        const uint32_t seen = seen_of(it.c0 + t * SK + 32 * sub);
+        if (active) {
+          if (seen != 0xffffffffu) { mask_unit(s0, seen, h); }
+          slot<0, true>(w, kr, vr, s0, s1, p1, p0, a.sc, st[last ? nxt : cur], last ? first : sub + 1, st[cur], sub, c,
+                        h, vlane);
+          if (seen != 0xffffffffu) { mask_unit(s1, seen, h); }
+        }
+        if (last && t + 2 < steps) {
+          write_stage<TYPE>(st[far], raw, tid);
+          if (t + 3 < steps) load_stage<TYPE>(raw, pid, a, src, it.c0 + (t + 3) * SK);
+          if (t + 4 < steps) page_ids<TYPE>(pid, a, src, it.c0 + (t + 4) * SK);
+        }
+        if (active)
+          slot<1, false>(w, kr, vr, s1, s0, p0, p1, a.sc, st[cur], 0, st[cur], 0, c, h, vlane);
+      }
+      cur = nxt;
+    }
+    if (active) {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) w.o[1][x & 3] = mfma32(vr[x], p1[x >> 2], w.o[1][x & 3]);
+    }
+    __syncthreads();
+  }
+  if (it.chunk == it.chunks - 1) {
+    const uint16_t* kb = (const uint16_t*)a.k.p + (int64_t)sq.row0 * a.k.ss + (int64_t)it.head * a.k.sh;
+    const uint16_t* vb = (const uint16_t*)a.v.p + (int64_t)sq.row0 * a.v.ss + (int64_t)it.head * a.v.sh;
+    for (int d0 = 0; d0 < sq.T; d0 += SK) {
+      int odd = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = tid / 16 + 16 * i, d = min(d0 + key, sq.T - 1);
+        const u32x4 kv = *reinterpret_cast<const u32x4*>(kb + (int64_t)d * a.k.ss + tid % 16 * 8);
+        const u32x4 vv = *reinterpret_cast<const u32x4*>(vb + (int64_t)d * a.v.ss + tid % 16 * 8);
+        u32x4 keep;
+        const u32x4 none = {};
+        odd |= not_finite(vv, keep);
+        *reinterpret_cast<u32x4*>(&st[0].k[key * TK + tid % 16 * 8]) = kv;
+        *reinterpret_cast<u32x4*>(&st[0].v[key * TV + tid % 16 * 8]) = d0 + key < sq.T ? keep : none;
+      }
+      odd = __syncthreads_or(odd);
+      for (int sub = wk; sub < 2; sub += WK) {
+        const int k0 = d0 + 32 * sub;
+        if (!active || k0 >= sq.T) continue;
+        uint32_t seen[2];
+#pragma unroll
+        for (int X = 0; X < 2; ++X) {
+          seen[X] = sq.T - k0 >= 32 ? 0xffffffffu : (1u << (sq.T - k0)) - 1;
+          if (a.mask) {
+            seen[X] &= a.mask[(int64_t)(sq.row0 + min(tok[X], sq.T - 1)) * (2 * a.mask_words) + (k0 >> 5)];
+          } else {
+            const int n = tok[X] + 1 - k0;
+            seen[X] &= n >= 32 ? 0xffffffffu : n > 0 ? (1u << n) - 1 : 0u;
+          }
+        }
+        unit_alone(w, 0, st[0], sub, seen[0], a.sc, c, h, vlane);
+        unit_alone(w, 1, st[0], sub, seen[1], a.sc, c, h, vlane);
+        if (odd) {                                         // flags in a stage of the wave's own
+          WaveTile& own = *reinterpret_cast<WaveTile*>(reinterpret_cast<char*>(&st[1]) + wave * sizeof(WaveTile));
+          static_assert(4 * sizeof(WaveTile) <= 2 * sizeof(Stage64), "the flags lie in two stages");
+          const uint16_t* v = vb + (int64_t)k0 * a.v.ss;
+          add_not_finite(w.o[0], own, v, a.v.ss, sq.T - k0, seen[0], h, vlane, lane);
+          add_not_finite(w.o[1], own, v, a.v.ss, sq.T - k0, seen[1], h, vlane, lane);
+        }
+      }
+      __syncthreads();
+    }
+  }
+
+  if constexpr (WK == 2) {                                 // the second key group's part joins the first's
+    float* buf = reinterpret_cast<float*>(st) + wr * (64 * OP + 256);
+    static_assert(sizeof(st) >= WR * (64 * OP + 256) * sizeof(float), "the join buffer lies in the stages");
+    float* ml = buf + 64 * OP;
+    if (wk == 1) {
+#pragma unroll
+      for (int X = 0; X < 2; ++X) {
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<float4*>(buf + (32 * X + c) * OP + 32 * dt + 8 * i + 4 * h) =
+                make_float4(w.o[X][dt][4 * i], w.o[X][dt][4 * i + 1], w.o[X][dt][4 * i + 2], w.o[X][dt][4 * i + 3]);
+        if (h == 0) {
+          ml[(32 * X + c) * 4] = w.m[X];
+          ml[(32 * X + c) * 4 + 1] = w.lo[X];
+          ml[(32 * X + c) * 4 + 2] = w.l[X];
+        }
+      }
+    }
+    __syncthreads();
+    if (wk == 1) return;
+#pragma unroll
+    for (int X = 0; X < 2; ++X) {
+      const float m1 = ml[(32 * X + c) * 4], m = fmaxf(w.m[X], m1);
+      const float f0 = w.m[X] == -INFINITY ? 0.0f : fast_exp2(w.m[X] - m);
+      const float f1 = m1 == -INFINITY ? 0.0f : fast_exp2(m1 - m);
+      w.m[X] = m;
+      w.lo[X] = w.lo[X] * f0 + ml[(32 * X + c) * 4 + 1] * f1;
+      w.l[X] = w.l[X] * f0 + ml[(32 * X + c) * 4 + 2] * f1;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 y = *reinterpret_cast<const float4*>(buf + (32 * X + c) * OP + 32 * dt + 8 * i + 4 * h);
+          w.o[X][dt][4 * i] = w.o[X][dt][4 * i] * f0 + y.x * f1;
+          w.o[X][dt][4 * i + 1] = w.o[X][dt][4 * i + 1] * f0 + y.y * f1;
+          w.o[X][dt][4 * i + 2] = w.o[X][dt][4 * i + 2] * f0 + y.z * f1;
+          w.o[X][dt][4 * i + 3] = w.o[X][dt][4 * i + 3] * f0 + y.w * f1;
+        }
+    }
+  }
+#pragma unroll
+  for (int X = 0; X < 2; ++X) {
+    if (tok[X] >= sq.T) continue;
+    const int row = row0 + 32 * X + c;
+    if (it.chunks == 1) {
+      const float lo = w.lo[X], inv = lo > 0.0f ? 1.0f / lo : lo == 0.0f ? 0.0f : lo;
+      const int head = it.head * a.g + row - tok[X] * a.g;
+      uint16_t* to = a.o + (int64_t)(sq.row0 + tok[X]) * a.o_ss + (int64_t)head * a.o_sh;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          bf16x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = (__bf16)(w.o[X][dt][4 * i + e] * inv);
+          *reinterpret_cast<bf16x4*>(to + 32 * dt + 8 * i + 4 * h) = y;
+        }
+      if (a.lse && h == 0)
+        a.lse[(int64_t)head * a.n_rows + sq.row0 + tok[X]] =
+            w.l[X] == 0.0f ? -INFINITY : (w.m[X] + fast_log2(w.l[X])) * LN2;
+    } else {
+      const int64_t at = (int64_t)blockIdx.x * ROWS + 64 * wr + 32 * X + c;
+      float* to = a.part_o + at * D;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<float4*>(to + 32 * dt + 8 * i + 4 * h) =
+              make_float4(w.o[X][dt][4 * i], w.o[X][dt][4 * i + 1], w.o[X][dt][4 * i + 2], w.o[X][dt][4 * i + 3]);
+      if (h == 0) *reinterpret_cast<float4*>(a.part_ml + at * 4) = make_float4(w.m[X], w.lo[X], w.l[X], 0.0f);
+    }
+  }
+}
+
 // Joins the partials of the sequences that were cut into chunks. Workgroup
 // (row of a sequence's rows, KV head and sequence): 8 groups of 32 lanes take
 // every eighth partial, 4 channels a lane, and meet in LDS.
@@ -542,8 +974,11 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
 TreeShape tree_shape(const mmi_tree& t, int Hkv, int cus) {
   TreeShape s{};
   const int g = t.Hq / Hkv;
-  s.rows = 32;
-  s.target = 2 * cus;
+  // up to 64 rows a head the cache's bytes bound the work (below); the wide
+  // tiles hold a compute unit each, two narrow ones share one
+  const int rows = t.max_rows * g;
+  s.rows = rows <= 64 ? 32 : rows <= 128 ? 128 : 256;
+  s.target = s.rows == 32 ? 2 * cus : cus;
   // tiles of all sequences, and `target` chunks more (each sequence's last chunk may be short)
   const int64_t most = (t.max_rows * (int64_t)g + s.rows - 1) / s.rows;
   const int64_t tiles = std::min<int64_t>(most * t.n_seq, ((int64_t)t.n_rows * g + (int64_t)t.n_seq * (s.rows - 1)) / s.rows);
@@ -559,19 +994,29 @@ TreeShape tree_shape(const mmi_tree& t, int Hkv, int cus) {
   return s;
 }
 
+template <int TYPE>
+static void launch_type(const TreeArgs& a, int rows, hipStream_t st) {
+  const dim3 grid((unsigned)a.items);
+  if (rows == 32) hipLaunchKernelGGL(k_tree<TYPE>, grid, dim3(256), 0, st, a);
+  else if (rows == 128) hipLaunchKernelGGL((k_tree_wide<TYPE, 2>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_tree_wide<TYPE, 4>), grid, dim3(256), 0, st, a);
+}
+
 hipError_t launch_tree(const TreeArgs& a, int type, int rows, hipStream_t st) {
   if (a.n_seq <= 0 || a.n_rows <= 0) return hipSuccess;
-  const dim3 grid((unsigned)a.items);
   switch (type) {
-    case MMI_CACHE_BF16: hipLaunchKernelGGL(k_tree<MMI_CACHE_BF16>, grid, dim3(256), 0, st, a); break;
-    case MMI_CACHE_FP8: hipLaunchKernelGGL(k_tree<MMI_CACHE_FP8>, grid, dim3(256), 0, st, a); break;
-    case MMI_CACHE_INT8: hipLaunchKernelGGL(k_tree<MMI_CACHE_INT8>, grid, dim3(256), 0, st, a); break;
-    case MMI_CACHE_FP4: hipLaunchKernelGGL(k_tree<MMI_CACHE_FP4>, grid, dim3(256), 0, st, a); break;
+    case MMI_CACHE_BF16: launch_type<MMI_CACHE_BF16>(a, rows, st); break;
+    case MMI_CACHE_FP8: launch_type<MMI_CACHE_FP8>(a, rows, st); break;
+    case MMI_CACHE_INT8: launch_type<MMI_CACHE_INT8>(a, rows, st); break;
+    case MMI_CACHE_FP4: launch_type<MMI_CACHE_FP4>(a, rows, st); break;
     default: return hipErrorInvalidValue;
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.max_len <= CHUNK) return e;   // one chunk a sequence at most
-  hipLaunchKernelGGL(k_tree_join<32>, dim3((unsigned)(a.max_rows * a.g * a.c.Hkv * a.n_seq)), dim3(256), 0, st, a);
+  const dim3 join((unsigned)(a.max_rows * a.g * a.c.Hkv * a.n_seq));
+  if (rows == 32) hipLaunchKernelGGL(k_tree_join<32>, join, dim3(256), 0, st, a);
+  else if (rows == 128) hipLaunchKernelGGL(k_tree_join<128>, join, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_tree_join<256>, join, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
