@@ -14,10 +14,6 @@ ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          # no packed-fp32 instructions from the compiler
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-# MFMA results in vector registers: left to itself the compiler gives a kernel
-# of more than 256 registers accumulators that the vector ALU cannot address,
-# and copies them back and forth in its loop
-FILE_FLAGS = {"k_tree.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _run(cmd):
@@ -44,7 +40,7 @@ def build(verbose: bool = False, asan: bool = False) -> str:
     objs = [os.path.join(obj_dir, f[:-4] + ".o") for f in srcs]
     jobs = min(len(srcs), int(os.environ.get("MAX_JOBS", "8")))
     with ThreadPoolExecutor(max_workers=max(1, jobs)) as ex:
-        futs = [ex.submit(_run, [hipcc, *FLAGS, *FILE_FLAGS.get(s, []), *extra, "-c", os.path.join(CSRC, s), "-o", o])
+        futs = [ex.submit(_run, [hipcc, *FLAGS, *extra, "-c", os.path.join(CSRC, s), "-o", o])
                 for s, o in zip(srcs, objs)]
         for f in futs:
             msg = f.result()

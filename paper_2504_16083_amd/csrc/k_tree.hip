@@ -54,7 +54,8 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Sum over the workgroup's 256 threads, and the sum before this thread.
+// Sum over the workgroup's NT threads, and the sum before this thread.
+template <int NT>
 __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* before, int64_t* sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int64_t s = x;
@@ -68,7 +69,7 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* before, int64_
   __syncthreads();
   int64_t base = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < NT / 64; ++w) {
     if (w < wave) base += sh[w];
     all += sh[w];
   }
@@ -84,26 +85,26 @@ struct Item {
 // Item `it` of the batch. The chunk length follows from the work of the whole
 // batch (cached tokens x tiles x heads, cut into `target` parts), so long
 // sequences get many chunks and short ones few, whatever the bounds were.
-template <int ROWS>
+template <int ROWS, int NT>
 __device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, int64_t* sh64, int* sh) {
   const int tid = threadIdx.x;
   int64_t work = 0, before;
-  for (int b = tid; b < a.n_seq; b += 256) {
+  for (int b = tid; b < a.n_seq; b += NT) {
     const Seq s = sequence(a, b);
     work += (int64_t)((s.T * a.g + ROWS - 1) / ROWS) * s.L;
   }
-  work = block_scan(work, &before, sh64) * a.c.Hkv;
+  work = block_scan<NT>(work, &before, sh64) * a.c.Hkv;
   const int64_t len = (work + a.target - 1) / a.target;
   const int chunk = (int)((max(len, (int64_t)1) + CHUNK - 1) / CHUNK * CHUNK);
   if (tid == 0) sh[0] = -1;
   int64_t base = 0;
-  for (int b0 = 0; b0 < a.n_seq; b0 += 256) {
+  for (int b0 = 0; b0 < a.n_seq; b0 += NT) {
     const int b = b0 + tid;
     Seq s = {0, 0, 0};
     if (b < a.n_seq) s = sequence(a, b);
     const int tiles = (s.T * a.g + ROWS - 1) / ROWS, chunks = max(1, (s.L + chunk - 1) / chunk);
     const int64_t n = (int64_t)tiles * a.c.Hkv * chunks;
-    const int64_t all = block_scan(n, &before, sh64);
+    const int64_t all = block_scan<NT>(n, &before, sh64);
     const int64_t at = it - base - before;
     if (n > 0 && at >= 0 && at < n) {
       const int tile = (int)(at % tiles), head = (int)(at / tiles % a.c.Hkv);
@@ -234,8 +235,8 @@ __device__ __forceinline__ float half_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-__device__ __forceinline__ bf16x8 v_operand(const WaveTile& t, int vlane, int half, int dt) {
-  const uint16_t* p = &t.v[vlane + 16 * half * TV + 32 * dt];
+__device__ __forceinline__ bf16x8 v_operand(const uint16_t* v, int vlane, int half, int dt) {
+  const uint16_t* p = v + vlane + 16 * half * TV + 32 * dt;
   const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p));
   const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p + 8 * TV));
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -284,7 +285,7 @@ __device__ __forceinline__ void attend(Rows& r, const WaveTile& t, uint32_t seen
 #pragma unroll
   for (int half = 0; half < 2; ++half)
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt) r.o[dt] = mfma32(v_operand(t, vlane, half, dt), p[half], r.o[dt]);
+    for (int dt = 0; dt < 4; ++dt) r.o[dt] = mfma32(v_operand(t.v, vlane, half, dt), p[half], r.o[dt]);
 }
 
 // Infinities and NaN in the V of drafted keys reach only the rows that see
@@ -292,7 +293,7 @@ __device__ __forceinline__ void attend(Rows& r, const WaveTile& t, uint32_t seen
 // staged without them, and here what they add is found from products of 0/1
 // flags, of the rows that see a key and of the channels where it holds +inf,
 // -inf or a NaN. v: V of the block's first key, n: its keys.
-__device__ __forceinline__ void add_not_finite(f32x16 (&o)[4], WaveTile& t, const uint16_t* v, int64_t ss, int n,
+__device__ __forceinline__ void add_not_finite(f32x16 (&o)[4], uint16_t* flags, const uint16_t* v, int64_t ss, int n,
                                                uint32_t seen, int h, int vlane, int lane) {
   bf16x8 flag[2];
 #pragma unroll
@@ -314,7 +315,7 @@ __device__ __forceinline__ void add_not_finite(f32x16 (&o)[4], WaveTile& t, cons
         }
         w[e] = f;
       }
-      *reinterpret_cast<u32x4*>(&t.v[(4 * i + lane / 16) * TV + lane % 16 * 8]) = w;
+      *reinterpret_cast<u32x4*>(flags + (4 * i + lane / 16) * TV + lane % 16 * 8) = w;
     }
     wave_fence();
     const float add = what == 2 ? __uint_as_float(0x7fc00000u) : what ? -INFINITY : INFINITY;
@@ -322,7 +323,7 @@ __device__ __forceinline__ void add_not_finite(f32x16 (&o)[4], WaveTile& t, cons
     for (int dt = 0; dt < 4; ++dt) {
       f32x16 n = {};
 #pragma unroll
-      for (int half = 0; half < 2; ++half) n = mfma32(v_operand(t, vlane, half, dt), flag[half], n);
+      for (int half = 0; half < 2; ++half) n = mfma32(v_operand(flags, vlane, half, dt), flag[half], n);
 #pragma unroll
       for (int x = 0; x < 16; ++x) o[dt][x] += n[x] > 0.0f ? add : 0.0f;
     }
@@ -338,7 +339,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   __shared__ int64_t sh64[4];
   __shared__ int sh[8];
   Item it;
-  if (!find_item<ROWS>(a, blockIdx.x, it, sh64, sh)) return;
+  if (!find_item<ROWS, 256>(a, blockIdx.x, it, sh64, sh)) return;
   const Seq sq = sequence(a, it.b);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int c = lane & 31, h = lane >> 5;
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
       wave_fence();
       attend(r, t, seen, a.sc, c, h, vlane);
       wave_fence();
-      if (odd) add_not_finite(r.o, t, vb + (int64_t)d0 * a.v.ss, a.v.ss, sq.T - d0, seen, h, vlane, lane);
+      if (odd) add_not_finite(r.o, t.v, vb + (int64_t)d0 * a.v.ss, a.v.ss, sq.T - d0, seen, h, vlane, lane);
     }
   }
 
@@ -485,20 +486,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 
 // ------------------------------------------------------------------ many rows
 // With more than 64 rows a head the products, not the cache's bytes, bound the
-// work, and a staged key has to serve as many rows as registers hold: a wave
-// has two tiles of 32 rows (512 registers, one wave a SIMD), so that every K
-// and V operand read from LDS feeds two MFMAs. The workgroup's four waves are
-// WR groups of rows times 4 / WR groups of keys; keys go through three LDS
-// stages of 64, one barrier a stage.
+// work: keys are staged once for all rows of a workgroup's tile. Its eight
+// waves (two a SIMD) are WR groups of 32 rows times 8 / WR groups of keys;
+// the keys go through four LDS stages of 64, one barrier a stage.
 //
-// A unit is 32 keys x 32 rows (one tile); a wave's units alternate its tiles.
-// Slot u issues QK of unit u + 1 and PV of unit u - 1 (8 MFMAs each, in turn)
-// with the softmax of unit u spread between them, since the vector ALU
-// overlaps only MFMAs of the same wave. Even slots (tile 0) use the operands
-// of a key block for the last time and read those of the next one into the
-// same registers behind each MFMA.
+// A unit is 32 keys against a wave's 32 rows. Slot u issues QK of unit u + 1
+// and PV of unit u - 1 (8 MFMAs each, in turn) with the softmax of unit u
+// spread between them, since the vector ALU overlaps only MFMAs of the same
+// wave; operands are read from LDS three MFMAs ahead. Two tiles a wave and
+// one wave a SIMD (512 registers, half the LDS reads) took 209 us where this
+// takes 168 us (64 drafts over 131072 tokens, 28 heads on 4): the compiler
+// moves what it keeps in the accumulator half back and forth.
 constexpr int SK = 64;                 // keys of a stage
-constexpr int NST = 3;
+constexpr int NST = 4;
+constexpr int NTW = 512;               // threads
 
 struct __align__(16) Stage64 {
   uint16_t k[SK * TK];
@@ -506,8 +507,10 @@ struct __align__(16) Stage64 {
 };
 
 template <int TYPE>
-struct Raw64 {                         // a thread's pieces of a stage: keys key0 + i * RP
-  static constexpr int CPR = Codec<TYPE>::ROW / 16, RP = 256 / CPR, N = SK / RP;
+struct Raw64 {                         // a thread's pieces of a stage: piece i is number tid + i * NTW
+  static constexpr int CPR = Codec<TYPE>::ROW / 16;        // pieces a row
+  static constexpr int N = SK * CPR / NTW > 0 ? SK * CPR / NTW : 1;
+  static constexpr int LIVE = SK * CPR < NTW ? SK * CPR : NTW;   // threads with pieces
   u32x4 k[N], v[N];
   uint32_t ks[N], vs[N];
   int ok[N];
@@ -519,12 +522,13 @@ struct KeySource {
 };
 
 template <int TYPE>
+__device__ __forceinline__ int key_of(int tid, int i) { return (tid % Raw64<TYPE>::LIVE + i * NTW) / Raw64<TYPE>::CPR; }
+
+template <int TYPE>
 __device__ __forceinline__ void page_ids(int (&p)[Raw64<TYPE>::N], const TreeArgs& a, const KeySource& s, int t0) {
 #pragma unroll
-  for (int i = 0; i < Raw64<TYPE>::N; ++i) {
-    const int t = t0 + s.tid / Raw64<TYPE>::CPR + i * Raw64<TYPE>::RP;
-    p[i] = s.pages[min(t, s.c1 - 1) >> a.c.shift];
-  }
+  for (int i = 0; i < Raw64<TYPE>::N; ++i)
+    p[i] = s.pages[min(t0 + key_of<TYPE>(s.tid, i), s.c1 - 1) >> a.c.shift];
 }
 
 template <int TYPE>
@@ -533,7 +537,7 @@ __device__ __forceinline__ void load_stage(Raw64<TYPE>& r, const int (&p)[Raw64<
   typedef Raw64<TYPE> R;
 #pragma unroll
   for (int i = 0; i < R::N; ++i) {
-    const int t = t0 + s.tid / R::CPR + i * R::RP;
+    const int t = t0 + key_of<TYPE>(s.tid, i);
     const bool there = (uint32_t)p[i] < (uint64_t)a.c.n_pages;
     r.ok[i] = there && t < s.c1;
     const int64_t page = there ? p[i] : 0;
@@ -552,34 +556,30 @@ __device__ __forceinline__ void load_stage(Raw64<TYPE>& r, const int (&p)[Raw64<
 template <int TYPE>
 __device__ __forceinline__ void write_stage(Stage64& st, const Raw64<TYPE>& r, int tid) {
   typedef Raw64<TYPE> R;
+  if (R::LIVE < NTW && tid >= R::LIVE) return;
 #pragma unroll
   for (int i = 0; i < R::N; ++i) {
-    const int key = tid / R::CPR + i * R::RP, piece = tid % R::CPR;
+    const int key = key_of<TYPE>(tid, i), piece = tid % R::CPR;
     const u32x4 none = {};
     put_piece<TYPE>(&st.k[key * TK], r.k[i], r.ks[i], piece);
+    // a key that does not exist weighs nothing, whatever its place in the page holds
     put_piece<TYPE>(&st.v[key * TV], r.ok[i] ? r.v[i] : none, r.ok[i] ? r.vs[i] : 0u, piece);
   }
 }
 
-struct Tiles {                         // a wave's 64 rows
-  f32x16 o[2][4];
-  bf16x8 q[2][8];
-  float m[2], l[2], lo[2];
-};
-
-__device__ __forceinline__ bf16x8 k_read(const Stage64& st, int sub, int x, int c, int h) {
-  return *reinterpret_cast<const bf16x8*>(&st.k[(32 * sub + c) * TK + h * 64 + x * 8]);
-}
-
-__device__ __forceinline__ bf16x8 v_read(const Stage64& st, int sub, int x, int vlane) {   // x: half, dt
-  const uint16_t* p = &st.v[vlane + (32 * sub + 16 * (x >> 2)) * TV + 32 * (x & 3)];
+// MFMA operand i of a slot: even ones K rows of the next unit, odd ones
+// transposed V of the last.
+__device__ __forceinline__ bf16x8 slot_operand(int i, const uint16_t* kp, const uint16_t* vp) {
+  const int x = i >> 1;
+  if ((i & 1) == 0) return *reinterpret_cast<const bf16x8*>(kp + x * 8);
+  const uint16_t* p = vp + 16 * (x >> 2) * TV + 32 * (x & 3);
   const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p));
   const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p + 8 * TV));
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 __device__ __forceinline__ void mask_unit(f32x16& s, uint32_t seen, int h) {
-  const uint32_t mine = seen >> (4 * h);
+  const uint32_t mine = seen >> (4 * h);     // element 4 i + j is key 8 i + 4 h + j
 #pragma unroll
   for (int x = 0; x < 16; ++x)
     if (!(mine >> (8 * (x >> 2) + (x & 3)) & 1)) s[x] = -INFINITY;
@@ -595,138 +595,132 @@ struct SoftState {
   float mx, base, alpha, rs, ro;
 };
 
-__device__ __forceinline__ void soft_piece(int piece, f32x16& s, float sc, float& m, float& l, float& lo,
-                                           bf16x8 (&p)[2], SoftState& z) {
+template <bool WL>
+__device__ __forceinline__ void soft_piece(int piece, f32x16& s, float sc, Rows& r, bf16x8 (&p)[2], SoftState& z) {
   if (piece < 2) {
     float mx = s[8 * piece];
 #pragma unroll
     for (int x = 1; x < 8; ++x) mx = fmaxf(mx, s[8 * piece + x]);
     z.mx = piece == 0 ? mx : fmaxf(z.mx, mx);
   } else if (piece == 2) {
-    const float mx = half_max(z.mx) * sc;
-    const bool move = __any(mx > m + SLACK);
-    const float mn = move ? fmaxf(m, mx) : m;
-    z.alpha = m == mn ? 1.0f : fast_exp2(m - mn);
-    m = mn;
-    z.base = mn == -INFINITY ? 0.0f : mn;
+    const float mx = half_max(z.mx) * sc;                  // sc > 0
+    const bool move = __any(mx > r.m + SLACK);
+    const float mn = move ? fmaxf(r.m, mx) : r.m;
+    z.alpha = r.m == mn ? 1.0f : fast_exp2(r.m - mn);
+    r.m = mn;
+    z.base = mn == -INFINITY ? 0.0f : mn;                  // nothing seen yet: every P is 2^-inf = 0
     z.rs = z.ro = 0.0f;
   } else if (piece < 19) {
     const int x = piece - 3;
     s[x] = fast_exp2(fmaf(s[x], sc, -z.base));
-    z.rs += s[x];
+    if (WL) z.rs += s[x];
   } else if (piece < 21) {
     const int half = piece - 19;
     const bf16e2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
-    for (int x = 0; x < 8; ++x) p[half][x] = (__bf16)s[8 * half + x];
+    for (int x = 0; x < 8; ++x) p[half][x] = (__bf16)s[8 * half + x];   // rounded for the product: O is divided by the sum of these
 #pragma unroll
     for (int x = 0; x < 4; ++x)
       z.ro = __builtin_amdgcn_fdot2_f32_bf16(bf16e2{p[half][2 * x], p[half][2 * x + 1]}, one, z.ro, false);
   } else {
-    l = l * z.alpha + half_sum(z.rs);
-    lo = lo * z.alpha + half_sum(z.ro);
+    if (WL) r.l = r.l * z.alpha + half_sum(z.rs);
+    r.lo = r.lo * z.alpha + half_sum(z.ro);
   }
 }
 
-// One slot: softmax of tile X's unit (scores s_sm), QK of the other tile's
-// next unit into s_qk, PV of the other tile's last unit. READ (even slots):
-// the K of the next key block and the V of this one follow their registers'
-// last use.
-template <int X, bool READ>
-__device__ __forceinline__ void slot(Tiles& w, bf16x8 (&kr)[8], bf16x8 (&vr)[8], f32x16& s_sm, f32x16& s_qk,
-                                     const bf16x8 (&p_pv)[2], bf16x8 (&p_sm)[2], float sc, const Stage64& knext,
-                                     int ksub, const Stage64& vnext, int vsub, int c, int h, int vlane) {
-  constexpr int Y = 1 - X;
+__device__ __forceinline__ void rescale(Rows& r, float alpha) {
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) r.o[dt][x] *= alpha;
+}
+
+template <bool WL>
+__device__ __forceinline__ void slot(Rows& r, f32x16& s_sm, f32x16& s_qk, const bf16x8 (&p_pv)[2], bf16x8 (&p_sm)[2],
+                                     float sc, const uint16_t* kp, const uint16_t* vp) {
+  constexpr int AHEAD = 3;
   SoftState z;
-  int pc = 0;
   const f32x16 zero = {};
+  bf16x8 op[AHEAD + 1];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) op[i] = slot_operand(i, kp, vp);
+  int pc = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
+    if (i + AHEAD < 16) op[(i + AHEAD) % (AHEAD + 1)] = slot_operand(i + AHEAD, kp, vp);
+    const bf16x8 av = op[i % (AHEAD + 1)];
     const int x = i >> 1;
-    if ((i & 1) == 0) {
-      s_qk = mfma32(kr[x], w.q[Y][x], x == 0 ? zero : s_qk);
-      if (READ) kr[x] = k_read(knext, ksub, x, c, h);
-    } else {
-      w.o[Y][x & 3] = mfma32(vr[x], p_pv[x >> 2], w.o[Y][x & 3]);
-      if (READ) vr[x] = v_read(vnext, vsub, x, vlane);
-    }
+    if ((i & 1) == 0) s_qk = mfma32(av, r.q[x], x == 0 ? zero : s_qk);
+    else r.o[x & 3] = mfma32(av, p_pv[x >> 2], r.o[x & 3]);
     const int end = (i + 1) * PIECES / 16;
 #pragma unroll
-    for (; pc < end; ++pc) soft_piece(pc, s_sm, sc, w.m[X], w.l[X], w.lo[X], p_sm, z);
+    for (; pc < end; ++pc) soft_piece<WL>(pc, s_sm, sc, r, p_sm, z);
     __builtin_amdgcn_sched_barrier(0);
   }
-  if (__any(z.alpha != 1.0f)) {
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) w.o[X][dt][x] *= z.alpha;
-  }
+  if (__any(z.alpha != 1.0f)) rescale(r, z.alpha);         // O holds PV up to unit u - 1, by the old maximum
 }
 
-// A staged block of 32 keys against one tile, nothing overlapped.
-__device__ __forceinline__ void unit_alone(Tiles& w, int X, const Stage64& st, int sub, uint32_t seen, float sc,
-                                           int c, int h, int vlane) {
+// A staged block of 32 keys, nothing overlapped.
+__device__ __forceinline__ void unit_alone(Rows& r, uint32_t seen, float sc, int h, const uint16_t* kp,
+                                           const uint16_t* vp) {
   f32x16 s = {};
 #pragma unroll
-  for (int x = 0; x < 8; ++x) s = mfma32(k_read(st, sub, x, c, h), w.q[X][x], s);
+  for (int x = 0; x < 8; ++x) s = mfma32(slot_operand(2 * x, kp, vp), r.q[x], s);
   mask_unit(s, seen, h);
   SoftState z;
   bf16x8 p[2];
 #pragma unroll
-  for (int pc = 0; pc < PIECES; ++pc) soft_piece(pc, s, sc, w.m[X], w.l[X], w.lo[X], p, z);
+  for (int pc = 0; pc < PIECES; ++pc) soft_piece<true>(pc, s, sc, r, p, z);
+  rescale(r, z.alpha);
 #pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-    for (int x = 0; x < 16; ++x) w.o[X][dt][x] *= z.alpha;
-#pragma unroll
-  for (int x = 0; x < 8; ++x) w.o[X][x & 3] = mfma32(v_read(st, sub, x, vlane), p[x >> 2], w.o[X][x & 3]);
+  for (int x = 0; x < 8; ++x) r.o[x & 3] = mfma32(slot_operand(2 * x + 1, kp, vp), p[x >> 2], r.o[x & 3]);
 }
 
-template <int TYPE, int WR>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_tree_wide(TreeArgs a) {
-  constexpr int ROWS = 64 * WR, WK = 4 / WR, SUBS = 2 / WK;   // rows a workgroup, key groups, a wave's blocks a stage
+template <int TYPE, int WR, bool WL>
+__global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k_tree_wide(TreeArgs a) {
+  constexpr int ROWS = 32 * WR, WK = 8 / WR;               // rows of a workgroup, groups of keys
+  static_assert(WK == 1 || WK == 2, "a stage holds two units");
   __shared__ Stage64 st[NST];
-  __shared__ int64_t sh64[4];
+  __shared__ int64_t sh64[8];
   __shared__ int sh[8];
   Item it;
-  if (!find_item<ROWS>(a, blockIdx.x, it, sh64, sh)) return;
+  if (!find_item<ROWS, NTW>(a, blockIdx.x, it, sh64, sh)) return;
   const Seq sq = sequence(a, it.b);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int wr = wave % WR, wk = wave / WR;
   const int c = lane & 31, h = lane >> 5;
+  // this lane's K row and transpose-read source inside a staged block of 32 keys
   const int grp = lane >> 4, li = lane & 15;
+  const int klane = c * TK + h * 64;
   const int vlane = (4 * (grp >> 1) + (li >> 2)) * TV + 16 * (grp & 1) + 4 * (li & 3);
-  const int row0 = it.tile * ROWS + 64 * wr;               // the wave's first row
-  const bool active = row0 < sq.T * a.g;
+  const int row = it.tile * ROWS + 32 * wr + c, tok = row / a.g;
+  const bool live = tok < sq.T;
+  const bool active = it.tile * ROWS + 32 * wr < sq.T * a.g;   // some row of the wave's is
 
-  Tiles w;
-  int tok[2];
-#pragma unroll
-  for (int X = 0; X < 2; ++X) {
-    const int row = row0 + 32 * X + c;
-    tok[X] = row / a.g;
-    const bool live = tok[X] < sq.T;
-    const uint16_t* q = (const uint16_t*)a.q.p + (int64_t)(sq.row0 + (live ? tok[X] : 0)) * a.q.ss +
-                        (int64_t)(it.head * a.g + (live ? row - tok[X] * a.g : 0)) * a.q.sh + h * 64;
+  Rows r;
+  {
+    const uint16_t* q = (const uint16_t*)a.q.p + (int64_t)(sq.row0 + (live ? tok : 0)) * a.q.ss +
+                        (int64_t)(it.head * a.g + (live ? row - tok * a.g : 0)) * a.q.sh + h * 64;
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
       const bf16x8 y = load16(q + 8 * x);
-      w.q[X][x] = live ? y : zero8();
+      r.q[x] = live ? y : zero8();
     }
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) w.o[X][dt][x] = 0.0f;
-    w.m[X] = -INFINITY;
-    w.l[X] = w.lo[X] = 0.0f;
   }
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) r.o[dt][x] = 0.0f;
+  r.m = -INFINITY;
+  r.l = r.lo = 0.0f;
 
-  const int steps = (it.c1 - it.c0 + SK - 1) / SK;
+  // stages, an even number of units a wave: what lies behind c1 is staged as nothing
+  const int steps = (it.c1 - it.c0 + SK * WK - 1) / (SK * WK) * WK;
   if (steps > 0) {
     const KeySource src = {a.pages + (int64_t)it.b * a.max_pages, it.head, it.c1, tid};
     // pages outside the cache are rare enough to ask once for the whole chunk
     int bad = 0;
-    for (int p = (it.c0 >> a.c.shift) + tid; p <= (it.c1 - 1) >> a.c.shift; p += 256)
+    for (int p = (it.c0 >> a.c.shift) + tid; p <= (it.c1 - 1) >> a.c.shift; p += NTW)
       bad |= (uint32_t)src.pages[p] >= (uint64_t)a.c.n_pages;
     const bool any_bad = __syncthreads_or(bad);
     auto seen_of = [&](int t0) -> uint32_t {               // keys of a block of 32 that exist
@@ -747,50 +741,53 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     load_stage<TYPE>(raw, pid, a, src, it.c0 + SK);
     page_ids<TYPE>(pid, a, src, it.c0 + 2 * SK);
     __syncthreads();
-    bf16x8 kr[8], vr[8], p0[2], p1[2];
+    // unit u: stage u / 2, block u % 2 (one key group), or stage u, block wk (two)
+    const int units = WK == 1 ? 2 * steps : steps;
+    auto k_at = [&](int u) -> const uint16_t* {
+      return st[(WK == 1 ? u >> 1 : u) & (NST - 1)].k + klane + 32 * TK * (WK == 1 ? u & 1 : wk);
+    };
+    auto v_at = [&](int u) -> const uint16_t* {
+      return st[(WK == 1 ? u >> 1 : u) & (NST - 1)].v + vlane + 32 * TV * (WK == 1 ? u & 1 : wk);
+    };
     f32x16 s0 = {}, s1 = {};
-    const int first = WK == 1 ? 0 : wk;                    // the wave's first block of a stage
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      kr[x] = k_read(st[0], first, x, c, h);
-      vr[x] = zero8();
-    }
+    bf16x8 p0[2], p1[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) p0[x] = p1[x] = zero8();
 #pragma unroll
-    for (int x = 0; x < 8; ++x) s0 = mfma32(kr[x], w.q[0][x], s0);
+    for (int x = 0; x < 8; ++x) s0 = mfma32(slot_operand(2 * x, k_at(0), nullptr), r.q[x], s0);
     write_stage<TYPE>(st[1], raw, tid);
     if (steps > 2) load_stage<TYPE>(raw, pid, a, src, it.c0 + 2 * SK);
     if (steps > 3) page_ids<TYPE>(pid, a, src, it.c0 + 3 * SK);
-    int cur = 0;
-    for (int t = 0; t < steps; ++t) {
-      const int nxt = cur == NST - 1 ? 0 : cur + 1, far = nxt == NST - 1 ? 0 : nxt + 1;
-#pragma unroll
-      for (int j = 0; j < SUBS; ++j) {
-        const int sub = WK == 1 ? j : wk;
-        const bool last = j == SUBS - 1;
-        // stage t + 1 is whole, and everybody is through with stage t - 1
-        if (last) __syncthreads();
-        const uint32_t seen = seen_of(it.c0 + t * SK + 32 * sub);
-        if (active) {
-          if (seen != 0xffffffffu) { mask_unit(s0, seen, h); }
-          slot<0, true>(w, kr, vr, s0, s1, p1, p0, a.sc, st[last ? nxt : cur], last ? first : sub + 1, st[cur], sub, c,
-                        h, vlane);
-          if (seen != 0xffffffffu) { mask_unit(s1, seen, h); }
-        }
-        if (last && t + 2 < steps) {
-          write_stage<TYPE>(st[far], raw, tid);
-          if (t + 3 < steps) load_stage<TYPE>(raw, pid, a, src, it.c0 + (t + 3) * SK);
-          if (t + 4 < steps) page_ids<TYPE>(pid, a, src, it.c0 + (t + 4) * SK);
-        }
-        if (active)
-          slot<1, false>(w, kr, vr, s1, s0, p0, p1, a.sc, st[cur], 0, st[cur], 0, c, h, vlane);
+    // The barrier before the last unit of stage t: stage t + 1 is whole, and
+    // every wave is through with the unit before, thus with stage t - 2 (and
+    // with one key group t - 1). The slot before unit 0 has no V yet: its P
+    // is zero, and unit 0's own block stands in for it.
+    auto stage_on = [&](int t) {
+      if (t + 2 >= steps) return;
+      write_stage<TYPE>(st[(t + 2) & (NST - 1)], raw, tid);
+      if (t + 3 < steps) load_stage<TYPE>(raw, pid, a, src, it.c0 + (t + 3) * SK);
+      if (t + 4 < steps) page_ids<TYPE>(pid, a, src, it.c0 + (t + 4) * SK);
+    };
+    for (int u = 0; u < units; u += 2) {
+      if (WK == 2) __syncthreads();
+      uint32_t seen = seen_of(it.c0 + (WK == 1 ? 32 * u : SK * u + 32 * wk));
+      if (active) {
+        if (seen != 0xffffffffu) mask_unit(s0, seen, h);
+        slot<WL>(r, s0, s1, p1, p0, a.sc, k_at(u + 1), v_at(u > 0 ? u - 1 : 0));
       }
-      cur = nxt;
+      if (WK == 2) stage_on(u);
+      __syncthreads();
+      seen = seen_of(it.c0 + (WK == 1 ? 32 * (u + 1) : SK * (u + 1) + 32 * wk));
+      if (active) {
+        if (seen != 0xffffffffu) mask_unit(s1, seen, h);
+        slot<WL>(r, s1, s0, p0, p1, a.sc, k_at(u + 2), v_at(u));
+      }
+      stage_on(WK == 1 ? u >> 1 : u + 1);
     }
     if (active) {
+      const uint16_t* vp = v_at(units - 1);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) w.o[1][x & 3] = mfma32(vr[x], p1[x >> 2], w.o[1][x & 3]);
+      for (int x = 0; x < 8; ++x) r.o[x & 3] = mfma32(slot_operand(2 * x + 1, nullptr, vp), p1[x >> 2], r.o[x & 3]);
     }
     __syncthreads();
   }
@@ -800,8 +797,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     for (int d0 = 0; d0 < sq.T; d0 += SK) {
       int odd = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = tid / 16 + 16 * i, d = min(d0 + key, sq.T - 1);
+      for (int i = 0; i < 2; ++i) {
+        const int key = tid / 16 + 32 * i, d = min(d0 + key, sq.T - 1);
         const u32x4 kv = *reinterpret_cast<const u32x4*>(kb + (int64_t)d * a.k.ss + tid % 16 * 8);
         const u32x4 vv = *reinterpret_cast<const u32x4*>(vb + (int64_t)d * a.v.ss + tid % 16 * 8);
         u32x4 keep;
@@ -814,25 +811,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
       for (int sub = wk; sub < 2; sub += WK) {
         const int k0 = d0 + 32 * sub;
         if (!active || k0 >= sq.T) continue;
-        uint32_t seen[2];
-#pragma unroll
-        for (int X = 0; X < 2; ++X) {
-          seen[X] = sq.T - k0 >= 32 ? 0xffffffffu : (1u << (sq.T - k0)) - 1;
-          if (a.mask) {
-            seen[X] &= a.mask[(int64_t)(sq.row0 + min(tok[X], sq.T - 1)) * (2 * a.mask_words) + (k0 >> 5)];
-          } else {
-            const int n = tok[X] + 1 - k0;
-            seen[X] &= n >= 32 ? 0xffffffffu : n > 0 ? (1u << n) - 1 : 0u;
-          }
+        uint32_t seen = sq.T - k0 >= 32 ? 0xffffffffu : (1u << (sq.T - k0)) - 1;
+        if (a.mask) {
+          seen &= a.mask[(int64_t)(sq.row0 + min(tok, sq.T - 1)) * (2 * a.mask_words) + (k0 >> 5)];
+        } else {
+          const int n = tok + 1 - k0;                      // keys k0 .. tok
+          seen &= n >= 32 ? 0xffffffffu : n > 0 ? (1u << n) - 1 : 0u;
         }
-        unit_alone(w, 0, st[0], sub, seen[0], a.sc, c, h, vlane);
-        unit_alone(w, 1, st[0], sub, seen[1], a.sc, c, h, vlane);
-        if (odd) {                                         // flags in a stage of the wave's own
-          WaveTile& own = *reinterpret_cast<WaveTile*>(reinterpret_cast<char*>(&st[1]) + wave * sizeof(WaveTile));
-          static_assert(4 * sizeof(WaveTile) <= 2 * sizeof(Stage64), "the flags lie in two stages");
-          const uint16_t* v = vb + (int64_t)k0 * a.v.ss;
-          add_not_finite(w.o[0], own, v, a.v.ss, sq.T - k0, seen[0], h, vlane, lane);
-          add_not_finite(w.o[1], own, v, a.v.ss, sq.T - k0, seen[1], h, vlane, lane);
+        unit_alone(r, seen, a.sc, h, st[0].k + klane + 32 * sub * TK, st[0].v + vlane + 32 * sub * TV);
+        if (odd) {                                         // flags in a place of the wave's own
+          uint16_t* own = st[1].k + wave * (KB * TV);
+          static_assert(8 * KB * TV * 2 <= 3 * sizeof(Stage64), "the flags lie in the other stages");
+          add_not_finite(r.o, own, vb + (int64_t)k0 * a.v.ss, a.v.ss, sq.T - k0, seen, h, vlane, lane);
         }
       }
       __syncthreads();
@@ -840,78 +830,67 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   }
 
   if constexpr (WK == 2) {                                 // the second key group's part joins the first's
-    float* buf = reinterpret_cast<float*>(st) + wr * (64 * OP + 256);
-    static_assert(sizeof(st) >= WR * (64 * OP + 256) * sizeof(float), "the join buffer lies in the stages");
-    float* ml = buf + 64 * OP;
+    float* buf = reinterpret_cast<float*>(st) + wr * (32 * OP + 128);
+    static_assert(sizeof(st) >= WR * (32 * OP + 128) * sizeof(float), "the join buffer lies in the stages");
+    float* ml = buf + 32 * OP;
     if (wk == 1) {
-#pragma unroll
-      for (int X = 0; X < 2; ++X) {
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<float4*>(buf + (32 * X + c) * OP + 32 * dt + 8 * i + 4 * h) =
-                make_float4(w.o[X][dt][4 * i], w.o[X][dt][4 * i + 1], w.o[X][dt][4 * i + 2], w.o[X][dt][4 * i + 3]);
-        if (h == 0) {
-          ml[(32 * X + c) * 4] = w.m[X];
-          ml[(32 * X + c) * 4 + 1] = w.lo[X];
-          ml[(32 * X + c) * 4 + 2] = w.l[X];
-        }
-      }
-    }
-    __syncthreads();
-    if (wk == 1) return;
-#pragma unroll
-    for (int X = 0; X < 2; ++X) {
-      const float m1 = ml[(32 * X + c) * 4], m = fmaxf(w.m[X], m1);
-      const float f0 = w.m[X] == -INFINITY ? 0.0f : fast_exp2(w.m[X] - m);
-      const float f1 = m1 == -INFINITY ? 0.0f : fast_exp2(m1 - m);
-      w.m[X] = m;
-      w.lo[X] = w.lo[X] * f0 + ml[(32 * X + c) * 4 + 1] * f1;
-      w.l[X] = w.l[X] * f0 + ml[(32 * X + c) * 4 + 2] * f1;
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 y = *reinterpret_cast<const float4*>(buf + (32 * X + c) * OP + 32 * dt + 8 * i + 4 * h);
-          w.o[X][dt][4 * i] = w.o[X][dt][4 * i] * f0 + y.x * f1;
-          w.o[X][dt][4 * i + 1] = w.o[X][dt][4 * i + 1] * f0 + y.y * f1;
-          w.o[X][dt][4 * i + 2] = w.o[X][dt][4 * i + 2] * f0 + y.z * f1;
-          w.o[X][dt][4 * i + 3] = w.o[X][dt][4 * i + 3] * f0 + y.w * f1;
-        }
-    }
-  }
-#pragma unroll
-  for (int X = 0; X < 2; ++X) {
-    if (tok[X] >= sq.T) continue;
-    const int row = row0 + 32 * X + c;
-    if (it.chunks == 1) {
-      const float lo = w.lo[X], inv = lo > 0.0f ? 1.0f / lo : lo == 0.0f ? 0.0f : lo;
-      const int head = it.head * a.g + row - tok[X] * a.g;
-      uint16_t* to = a.o + (int64_t)(sq.row0 + tok[X]) * a.o_ss + (int64_t)head * a.o_sh;
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          bf16x4 y;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = (__bf16)(w.o[X][dt][4 * i + e] * inv);
-          *reinterpret_cast<bf16x4*>(to + 32 * dt + 8 * i + 4 * h) = y;
-        }
-      if (a.lse && h == 0)
-        a.lse[(int64_t)head * a.n_rows + sq.row0 + tok[X]] =
-            w.l[X] == 0.0f ? -INFINITY : (w.m[X] + fast_log2(w.l[X])) * LN2;
-    } else {
-      const int64_t at = (int64_t)blockIdx.x * ROWS + 64 * wr + 32 * X + c;
-      float* to = a.part_o + at * D;
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<float4*>(to + 32 * dt + 8 * i + 4 * h) =
-              make_float4(w.o[X][dt][4 * i], w.o[X][dt][4 * i + 1], w.o[X][dt][4 * i + 2], w.o[X][dt][4 * i + 3]);
-      if (h == 0) *reinterpret_cast<float4*>(a.part_ml + at * 4) = make_float4(w.m[X], w.lo[X], w.l[X], 0.0f);
+          *reinterpret_cast<float4*>(buf + c * OP + 32 * dt + 8 * i + 4 * h) =
+              make_float4(r.o[dt][4 * i], r.o[dt][4 * i + 1], r.o[dt][4 * i + 2], r.o[dt][4 * i + 3]);
+      if (h == 0) {
+        ml[c * 4] = r.m;
+        ml[c * 4 + 1] = r.lo;
+        ml[c * 4 + 2] = r.l;
+      }
     }
+    __syncthreads();
+    if (wk == 1) return;
+    const float m1 = ml[c * 4], m = fmaxf(r.m, m1);
+    const float f0 = r.m == -INFINITY ? 0.0f : fast_exp2(r.m - m);
+    const float f1 = m1 == -INFINITY ? 0.0f : fast_exp2(m1 - m);
+    r.m = m;
+    r.lo = r.lo * f0 + ml[c * 4 + 1] * f1;
+    r.l = r.l * f0 + ml[c * 4 + 2] * f1;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 y = *reinterpret_cast<const float4*>(buf + c * OP + 32 * dt + 8 * i + 4 * h);
+        r.o[dt][4 * i] = r.o[dt][4 * i] * f0 + y.x * f1;
+        r.o[dt][4 * i + 1] = r.o[dt][4 * i + 1] * f0 + y.y * f1;
+        r.o[dt][4 * i + 2] = r.o[dt][4 * i + 2] * f0 + y.z * f1;
+        r.o[dt][4 * i + 3] = r.o[dt][4 * i + 3] * f0 + y.w * f1;
+      }
+  }
+  if (!live) return;
+  if (it.chunks == 1) {
+    const float inv = r.lo > 0.0f ? 1.0f / r.lo : r.lo == 0.0f ? 0.0f : r.lo;
+    const int head = it.head * a.g + row - tok * a.g;
+    uint16_t* to = a.o + (int64_t)(sq.row0 + tok) * a.o_ss + (int64_t)head * a.o_sh;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        bf16x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (__bf16)(r.o[dt][4 * i + e] * inv);
+        *reinterpret_cast<bf16x4*>(to + 32 * dt + 8 * i + 4 * h) = y;
+      }
+    if (WL && h == 0)
+      a.lse[(int64_t)head * a.n_rows + sq.row0 + tok] = r.l == 0.0f ? -INFINITY : (r.m + fast_log2(r.l)) * LN2;
+  } else {
+    const int64_t at = (int64_t)blockIdx.x * ROWS + 32 * wr + c;
+    float* to = a.part_o + at * D;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(to + 32 * dt + 8 * i + 4 * h) =
+            make_float4(r.o[dt][4 * i], r.o[dt][4 * i + 1], r.o[dt][4 * i + 2], r.o[dt][4 * i + 3]);
+    if (h == 0) *reinterpret_cast<float4*>(a.part_ml + at * 4) = make_float4(r.m, r.lo, r.l, 0.0f);
   }
 }
 
@@ -998,8 +977,10 @@ template <int TYPE>
 static void launch_type(const TreeArgs& a, int rows, hipStream_t st) {
   const dim3 grid((unsigned)a.items);
   if (rows == 32) hipLaunchKernelGGL(k_tree<TYPE>, grid, dim3(256), 0, st, a);
-  else if (rows == 128) hipLaunchKernelGGL((k_tree_wide<TYPE, 2>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_tree_wide<TYPE, 4>), grid, dim3(256), 0, st, a);
+  else if (rows == 128 && a.lse) hipLaunchKernelGGL((k_tree_wide<TYPE, 4, true>), grid, dim3(NTW), 0, st, a);
+  else if (rows == 128) hipLaunchKernelGGL((k_tree_wide<TYPE, 4, false>), grid, dim3(NTW), 0, st, a);
+  else if (a.lse) hipLaunchKernelGGL((k_tree_wide<TYPE, 8, true>), grid, dim3(NTW), 0, st, a);
+  else hipLaunchKernelGGL((k_tree_wide<TYPE, 8, false>), grid, dim3(NTW), 0, st, a);
 }
 
 hipError_t launch_tree(const TreeArgs& a, int type, int rows, hipStream_t st) {
