@@ -76,34 +76,43 @@ def lib():
 
 def _stream(ctx, stream):
     if stream is None:
-        stream = torch.cuda.current_stream(ctx.device)
+        return torch._C._cuda_getCurrentRawStream(ctx.device)    # current_stream() without its object
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+_BF16 = torch.bfloat16
+
+
 def _rows(ctx, name, t, n, heads):
-    """A [n, heads, 128] bfloat16 tensor on the context's device; its strides."""
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[2] != D:
+    """Strides of a [n, heads, 128] bfloat16 tensor on the context's device."""
+    # one pass over what is right; the reasons are looked for only where something is wrong
+    if t.dtype is _BF16 and t.get_device() == ctx.device and t.dim() == 3:
+        rows, h, d = t.shape
+        if d == D and (n is None or rows == n) and (heads is None or h == heads):
+            ss, sh, sd = t.stride()
+            if sd == 1:
+                # torch leaves the stride of a dimension of one entry open
+                if h == 1:
+                    sh = D
+                if rows <= 1:
+                    ss = max(sh * h, D)
+                return ss, sh
+            raise ValueError(f"the last dimension of {name} must be contiguous")
+    if t.dtype != _BF16 or t.dim() != 3 or t.shape[2] != D:
         raise ValueError(f"{name} must be a bfloat16 tensor [tokens, heads, {D}]")
-    if (n is not None and t.shape[0] != n) or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, [{n}, {heads}, {D}] expected")
-    if t.device.type != "cuda" or t.device.index != ctx.device:
+    _here(ctx, name, t)
+    raise ValueError(f"{name} has shape {tuple(t.shape)}, [{n}, {heads}, {D}] expected")
+
+
+def _here(ctx, name, t):
+    if t.get_device() != ctx.device:
         raise ValueError(f"{name} is on {t.device}, the context on device {ctx.device}")
-    ss, sh, sd = t.stride()
-    if sd != 1:
-        raise ValueError(f"the last dimension of {name} must be contiguous")
-    # torch leaves the stride of a dimension of one entry open
-    if t.shape[1] == 1:
-        sh = D
-    if t.shape[0] <= 1:
-        ss = max(sh * t.shape[1], D)
-    return ss, sh
 
 
 def _array(ctx, name, t, dtype, shape):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
-    if t.device.type != "cuda" or t.device.index != ctx.device:
-        raise ValueError(f"{name} is on {t.device}, the context on device {ctx.device}")
+    _here(ctx, name, t)
     return t.data_ptr()
 
 
@@ -183,7 +192,7 @@ class Cache:
         self.n_pages, self.Hkv, self.page = k.shape[:3]
         want = (self.n_pages, self.Hkv, self.page)
         bf16 = type == "bf16"
-        self.device = k.device
+        self.device, self.index = k.device, k.get_device()
         row = D if bf16 else ROW_BYTES[type]
         stride = self._pool("k", k, torch.bfloat16 if bf16 else torch.uint8, want + (row,))
         if self._pool("v", v, torch.bfloat16 if bf16 else torch.uint8, want + (row,)) != stride:
@@ -223,7 +232,7 @@ class Cache:
 
 
 def _on(ctx, cache):
-    if cache.device.type != "cuda" or cache.device.index != ctx.device:
+    if cache.index != ctx.device:
         raise ValueError(f"the cache is on {cache.device}, the context on device {ctx.device}")
 
 
