@@ -2,17 +2,16 @@
 //
 // The query rows of a KV head are (drafted token, query head of its group):
 // row r of sequence b is token r / g, head r % g. A workgroup takes a tile of
-// 32 of them and a chunk of the sequence's cached tokens; the last chunk also
-// takes the drafted tokens. Its four waves split the keys: each takes every
-// fourth block of 32 keys, stages it in LDS of its own (no barriers in the
-// loop) as bfloat16 whatever the cache's type, and keeps an online softmax:
-//   S^T (32 keys x 32 rows) = K Q^T           8 MFMA 32x32x16 bf16
-//   P = 2^(S - m), running maximum m and sums in fp32
-//   O^T (128 x 32) += V^T P^T                 8 MFMA 32x32x16 bf16
-// S^T has one row a lane, so its maximum and sum are in-lane but for one
-// exchange of halves, and P is already the operand of the second product.
-// At the end the waves' O, m and sums meet in LDS; a sequence of several
-// chunks leaves partials that k_tree_join merges in a fixed order.
+// them and a chunk of the sequence's cached tokens; the last chunk also takes
+// the drafted tokens. Every type is turned into bfloat16 on the way to the
+// matrix cores; a row keeps an online softmax over blocks of 32 keys:
+//   S^T (keys x rows) = K Q^T, P = 2^(S - m) with a running maximum m,
+//   O^T (128 x rows) += V^T P^T, sums of P in fp32.
+// S^T has one row a lane, so P is already the operand of the second product
+// (the keys of its contraction in the order that the lanes hold them).
+// Up to 32 rows a head the cache's bytes bound the work (k_tree_few), with
+// more the products (k_tree_wide). A sequence of several chunks leaves
+// partials that k_tree_join merges in a fixed order.
 #include <algorithm>
 
 #include "cache.hpp"
@@ -25,11 +24,6 @@ constexpr int TK = 136, TV = 160;      // bf16 a staged K / V row: operand reads
 constexpr int OP = 132;                // floats a row of the join buffer
 constexpr float SLACK = 8.0f;          // the maximum moves when a block's passes it by this (log2 units)
 constexpr int CHUNK = 128;             // chunks are multiples of a step of the four waves
-
-struct __align__(16) WaveTile {
-  uint16_t k[KB * TK];
-  uint16_t v[KB * TV];
-};
 
 typedef __attribute__((address_space(3))) bf16x4 lds4;
 
@@ -132,49 +126,6 @@ __device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, in
   return r.b >= 0;
 }
 
-// A block of 32 cached keys in registers, as its 16-byte pieces lie in the
-// cache: piece i of a lane belongs to key i * RP + lane / CPR.
-template <int TYPE>
-struct Raw {
-  static constexpr int CPR = Codec<TYPE>::ROW / 16;   // pieces a row
-  static constexpr int RP = 64 / CPR;                 // rows a wave-wide load
-  static constexpr int N = KB / RP;
-  u32x4 k[N], v[N];
-  uint32_t ks[N], vs[N];
-  uint32_t seen;                                      // keys that exist
-};
-
-template <int TYPE>
-__device__ __forceinline__ void load_block(Raw<TYPE>& r, const TreeArgs& a, const int32_t* pages, int head, int t0,
-                                           int len, int lane) {
-  typedef Raw<TYPE> R;
-  r.seen = len - t0 >= KB ? 0xffffffffu : (1u << (len - t0)) - 1;
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {              // 16 keys lie in one page
-    const int t = t0 + 16 * half;
-    const int p = t < len ? pages[t >> a.c.shift] : -1;
-    const bool ok = (uint32_t)p < (uint64_t)a.c.n_pages;
-    if (!ok) r.seen &= half ? 0x0000ffffu : 0xffff0000u;
-    const int64_t page = ok ? p : 0;
-    const int64_t in = ((int64_t)head << a.c.shift) + (t & ((1 << a.c.shift) - 1));
-    const uint8_t* kp = a.c.k + page * a.c.page_stride + in * Codec<TYPE>::ROW;
-    const uint8_t* vp = a.c.v + page * a.c.page_stride + in * Codec<TYPE>::ROW;
-    const uint32_t* ksp = Codec<TYPE>::SCALED ? (const uint32_t*)((const uint8_t*)a.c.ks + page * a.c.scale_stride) + in : nullptr;
-    const uint32_t* vsp = Codec<TYPE>::SCALED ? (const uint32_t*)((const uint8_t*)a.c.vs + page * a.c.scale_stride) + in : nullptr;
-#pragma unroll
-    for (int i = half * R::N / 2; i < (half + 1) * R::N / 2; ++i) {
-      const int row = (i - half * R::N / 2) * R::RP + lane / R::CPR;
-      const int off = row * Codec<TYPE>::ROW + lane % R::CPR * 16;
-      r.k[i] = *reinterpret_cast<const u32x4*>(kp + off);
-      r.v[i] = *reinterpret_cast<const u32x4*>(vp + off);
-      if constexpr (Codec<TYPE>::SCALED) {
-        r.ks[i] = ksp[row];
-        r.vs[i] = vsp[row];
-      }
-    }
-  }
-}
-
 // One 16-byte piece as bfloat16 into a staged row.
 template <int TYPE>
 __device__ __forceinline__ void put_piece(uint16_t* to, u32x4 w, uint32_t scales, int piece) {
@@ -189,20 +140,6 @@ __device__ __forceinline__ void put_piece(uint16_t* to, u32x4 w, uint32_t scales
       *reinterpret_cast<bf16x8*>(to + piece * 16) = decode8<TYPE>(w[0], w[1], s);
       *reinterpret_cast<bf16x8*>(to + piece * 16 + 8) = decode8<TYPE>(w[2], w[3], s);
     }
-  }
-}
-
-template <int TYPE>
-__device__ __forceinline__ void stage_block(WaveTile& t, const Raw<TYPE>& r, int lane) {
-  typedef Raw<TYPE> R;
-#pragma unroll
-  for (int i = 0; i < R::N; ++i) {
-    const int row = i * R::RP + lane / R::CPR, piece = lane % R::CPR;
-    put_piece<TYPE>(&t.k[row * TK], r.k[i], r.ks[i], piece);
-    // a key that does not exist weighs nothing, whatever its place in the page holds
-    const bool ok = r.seen >> row & 1;
-    const u32x4 none = {};
-    put_piece<TYPE>(&t.v[row * TV], ok ? r.v[i] : none, ok ? r.vs[i] : 0u, piece);
   }
 }
 
@@ -222,7 +159,7 @@ __device__ __forceinline__ bool not_finite(u32x4 w, u32x4& keep) {
 struct Rows {                          // a wave's 32 rows
   f32x16 o[4];
   bf16x8 q[8];
-  float m, l, lo;                      // running maximum (log2 units), sums of the fp32 and of the bf16 P
+  float m, l, lo;                      // maximum (log2 units) of a row; sums of this lane's P (fp32, bf16)
 };
 
 __device__ __forceinline__ float half_max(float x) {
@@ -242,99 +179,264 @@ __device__ __forceinline__ bf16x8 v_operand(const uint16_t* v, int vlane, int ha
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// The staged block against the wave's rows; bit k of `seen`: this lane's row
-// sees key k.
-__device__ __forceinline__ void attend(Rows& r, const WaveTile& t, uint32_t seen, float sc, int c, int h, int vlane) {
-  f32x16 s = {};
-#pragma unroll
-  for (int x = 0; x < 8; ++x)
-    s = mfma32(*reinterpret_cast<const bf16x8*>(&t.k[c * TK + h * 64 + x * 8]), r.q[x], s);
-  if (__any(seen != 0xffffffffu)) {
-    const uint32_t mine = seen >> (4 * h);   // element 4 i + j is key 8 i + 4 h + j
-#pragma unroll
-    for (int x = 0; x < 16; ++x)
-      if (!(mine >> (8 * (x >> 2) + (x & 3)) & 1)) s[x] = -INFINITY;
-  }
-  float mx = s[0];
-#pragma unroll
-  for (int x = 1; x < 16; ++x) mx = fmaxf(mx, s[x]);
-  mx = half_max(mx) * sc;                  // sc > 0
-  if (__any(mx > r.m + SLACK)) {
-    const float m = fmaxf(r.m, mx), alpha = r.m == m ? 1.0f : fast_exp2(r.m - m);
-    r.m = m;
-    r.l *= alpha;
-    r.lo *= alpha;
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) r.o[dt][x] *= alpha;
-  }
-  const float base = r.m == -INFINITY ? 0.0f : r.m;   // nothing seen yet: every P below is 2^-inf = 0
-  float rs = 0.0f, ro = 0.0f;
-  bf16x8 p[2];
-#pragma unroll
-  for (int x = 0; x < 16; ++x) {
-    const float e = fast_exp2(fmaf(s[x], sc, -base));
-    rs += e;
-    const __bf16 b = (__bf16)e;            // rounded for the product; O is divided by the sum of these
-    p[x >> 3][x & 7] = b;
-    ro += (float)b;
-  }
-  r.l += half_sum(rs);
-  r.lo += half_sum(ro);
-#pragma unroll
-  for (int half = 0; half < 2; ++half)
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt) r.o[dt] = mfma32(v_operand(t.v, vlane, half, dt), p[half], r.o[dt]);
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16e2;
+
+// Drafted keys d0 .. d0 + 31 that a row of token `tok` sees.
+__device__ __forceinline__ uint32_t seen_drafts(const TreeArgs& a, const Seq& sq, int tok, int d0) {
+  const uint32_t seen = sq.T - d0 >= KB ? 0xffffffffu : (1u << (sq.T - d0)) - 1;
+  if (a.mask) return seen & a.mask[(int64_t)(sq.row0 + min(tok, sq.T - 1)) * (2 * a.mask_words) + (d0 >> 5)];
+  const int n = tok + 1 - d0;                // keys d0 .. tok
+  return seen & (n >= KB ? 0xffffffffu : n > 0 ? (1u << n) - 1 : 0u);
 }
 
 // Infinities and NaN in the V of drafted keys reach only the rows that see
 // them (a product over the block would spread them as 0 x inf): the block was
 // staged without them, and here what they add is found from products of 0/1
-// flags, of the rows that see a key and of the channels where it holds +inf,
-// -inf or a NaN. v: V of the block's first key, n: its keys.
+// flags, of the rows that see a key and of the channels where it holds +inf
+// (what 0), -inf (1) or a NaN (2). v: V of the block's first key, n: its keys.
+__device__ __forceinline__ void flag_not_finite(uint16_t* flags, const uint16_t* v, int64_t ss, int n, int what,
+                                                int lane) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const u32x4 raw = *reinterpret_cast<const u32x4*>(v + (int64_t)min(4 * i + lane / 16, n - 1) * ss + lane % 16 * 8);
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t f = 0;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const uint32_t u = raw[e] >> (16 * s) & 0xffff;
+        const bool hit = what == 2 ? (u & 0x7fff) > 0x7f80 : u == (what ? 0xff80u : 0x7f80u);
+        f |= hit ? 0x3f80u << (16 * s) : 0u;
+      }
+      w[e] = f;
+    }
+    *reinterpret_cast<u32x4*>(flags + (4 * i + lane / 16) * TV + lane % 16 * 8) = w;
+  }
+}
+
 __device__ __forceinline__ void add_not_finite(f32x16 (&o)[4], uint16_t* flags, const uint16_t* v, int64_t ss, int n,
                                                uint32_t seen, int h, int vlane, int lane) {
-  bf16x8 flag[2];
+  bf16x8 sees[2];
 #pragma unroll
   for (int x = 0; x < 16; ++x)
-    flag[x >> 3][x & 7] = (__bf16)((seen >> (8 * (x >> 2) + 4 * h + (x & 3)) & 1) ? 1.0f : 0.0f);
-  for (int what = 0; what < 3; ++what) {   // +inf, -inf, NaN
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const u32x4 raw = *reinterpret_cast<const u32x4*>(v + (int64_t)min(4 * i + lane / 16, n - 1) * ss + lane % 16 * 8);
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        uint32_t f = 0;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const uint32_t u = raw[e] >> (16 * s) & 0xffff;
-          const bool hit = what == 2 ? (u & 0x7fff) > 0x7f80 : u == (what ? 0xff80u : 0x7f80u);
-          f |= hit ? 0x3f80u << (16 * s) : 0u;
-        }
-        w[e] = f;
-      }
-      *reinterpret_cast<u32x4*>(flags + (4 * i + lane / 16) * TV + lane % 16 * 8) = w;
-    }
+    sees[x >> 3][x & 7] = (__bf16)((seen >> (8 * (x >> 2) + 4 * h + (x & 3)) & 1) ? 1.0f : 0.0f);
+  for (int what = 0; what < 3; ++what) {
+    flag_not_finite(flags, v, ss, n, what, lane);
     wave_fence();
     const float add = what == 2 ? __uint_as_float(0x7fc00000u) : what ? -INFINITY : INFINITY;
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) {
-      f32x16 n = {};
+      f32x16 c = {};
 #pragma unroll
-      for (int half = 0; half < 2; ++half) n = mfma32(v_operand(flags, vlane, half, dt), flag[half], n);
+      for (int half = 0; half < 2; ++half) c = mfma32(v_operand(flags, vlane, half, dt), sees[half], c);
 #pragma unroll
-      for (int x = 0; x < 16; ++x) o[dt][x] += n[x] > 0.0f ? add : 0.0f;
+      for (int x = 0; x < 16; ++x) o[dt][x] += c[x] > 0.0f ? add : 0.0f;
     }
     wave_fence();
   }
 }
 
+// ------------------------------------------------------------------ few rows
+// Up to 32 rows: RN tiles of 16. The four waves of a workgroup split the keys:
+// each takes every fourth block of 32 and shares nothing until the end, so the
+// loop has no barrier. The MFMAs are 16x16x32 (a decoded token with its 4 to
+// 16 query heads fills a third of a 32-wide tile at most): lane (r = l % 16,
+// q = l / 16) holds row r of an operand and 8 of its 32 contracted entries.
+// K comes from the cache straight into that layout (64 contiguous bytes of a
+// row a load; which channels an MFMA contracts does not matter, Q follows);
+// only V goes through LDS, to be read transposed. Three workgroups a compute
+// unit keep about 100 KB of loads in flight.
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// First channel of lane group q's eight in MFMA x of QK.
 template <int TYPE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_tree(TreeArgs a) {
-  constexpr int ROWS = 32;
-  __shared__ WaveTile tiles[4];
+__device__ __forceinline__ int channel(int x, int q) {
+  return TYPE == MMI_CACHE_BF16 ? 32 * x + 8 * q : TYPE == MMI_CACHE_FP4 ? 32 * q + 8 * x : 64 * (x >> 1) + 16 * q + 8 * (x & 1);
+}
+
+template <int TYPE>
+struct Raw32 {                                        // a block of 32 keys as it lies in the cache
+  static constexpr int KN = Codec<TYPE>::ROW / 64;    // K pieces of a lane and tile of 16 keys
+  static constexpr int CPR = Codec<TYPE>::ROW / 16, RP = 64 / CPR, N = KB / RP;   // V: piece i = key i * RP + lane / CPR
+  u32x4 k[2][KN], v[N];
+  uint32_t ks[2], vs[N];
+  uint32_t seen;                                      // keys that exist
+};
+
+template <int TYPE>
+__device__ __forceinline__ void load_block(Raw32<TYPE>& r, const TreeArgs& a, const int32_t* pages, int head, int t0,
+                                           int len, int lane) {
+  typedef Raw32<TYPE> R;
+  r.seen = len - t0 >= KB ? 0xffffffffu : (1u << (len - t0)) - 1;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {              // 16 keys lie in one page
+    const int t = t0 + 16 * half;
+    const int p = t < len ? pages[t >> a.c.shift] : -1;
+    const bool ok = (uint32_t)p < (uint64_t)a.c.n_pages;
+    if (!ok) r.seen &= half ? 0x0000ffffu : 0xffff0000u;
+    const int64_t page = ok ? p : 0;
+    const int64_t in = ((int64_t)head << a.c.shift) + (t & ((1 << a.c.shift) - 1));
+    const uint8_t* kp = a.c.k + page * a.c.page_stride + in * Codec<TYPE>::ROW;
+    const uint8_t* vp = a.c.v + page * a.c.page_stride + in * Codec<TYPE>::ROW;
+#pragma unroll
+    for (int j = 0; j < R::KN; ++j)
+      r.k[half][j] = *reinterpret_cast<const u32x4*>(kp + (lane & 15) * Codec<TYPE>::ROW + 64 * j + 16 * (lane >> 4));
+#pragma unroll
+    for (int i = half * R::N / 2; i < (half + 1) * R::N / 2; ++i)
+      r.v[i] = *reinterpret_cast<const u32x4*>(vp + ((i - half * R::N / 2) * R::RP * R::CPR + lane) * 16);
+    if constexpr (Codec<TYPE>::SCALED) {
+      const uint32_t* ks = (const uint32_t*)((const uint8_t*)a.c.ks + page * a.c.scale_stride) + in;
+      const uint32_t* vs = (const uint32_t*)((const uint8_t*)a.c.vs + page * a.c.scale_stride) + in;
+      r.ks[half] = ks[lane & 15];
+#pragma unroll
+      for (int i = half * R::N / 2; i < (half + 1) * R::N / 2; ++i)
+        r.vs[i] = vs[(i - half * R::N / 2) * R::RP + lane / R::CPR];
+    }
+  }
+}
+
+// V of the block, transposed on the way out: [key][TV].
+template <int TYPE>
+__device__ __forceinline__ void stage_v(uint16_t* v, const Raw32<TYPE>& r, int lane) {
+  typedef Raw32<TYPE> R;
+#pragma unroll
+  for (int i = 0; i < R::N; ++i) {
+    const int key = i * R::RP + lane / R::CPR;
+    // a key that does not exist weighs nothing, whatever its place in the page holds
+    const bool ok = r.seen >> key & 1;
+    const u32x4 none = {};
+    put_piece<TYPE>(v + key * TV, ok ? r.v[i] : none, ok ? r.vs[i] : 0u, lane % R::CPR);
+  }
+}
+
+// The K operands of one tile of 16 keys.
+template <int TYPE>
+__device__ __forceinline__ void k_operands(bf16x8 (&op)[4], const Raw32<TYPE>& r, int half, int q) {
+  if constexpr (TYPE == MMI_CACHE_BF16) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) op[x] = __builtin_bit_cast(bf16x8, r.k[half][x]);
+  } else if constexpr (TYPE == MMI_CACHE_FP4) {
+    const float s = scale_value(r.ks[half] >> (8 * q) & 255);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) op[x] = decode4(r.k[half][0][x], s);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float s = scale_value(r.ks[half] >> (8 * (2 * j + (q >> 1))) & 255);
+      op[2 * j] = decode8<TYPE>(r.k[half][j][0], r.k[half][j][1], s);
+      op[2 * j + 1] = decode8<TYPE>(r.k[half][j][2], r.k[half][j][3], s);
+    }
+  }
+}
+
+template <int RN>
+struct FewRows {                       // a wave's RN tiles of 16 rows
+  f32x4 o[RN][8];
+  bf16x8 q[RN][4];
+  float m[RN], l[RN], lo[RN];          // maximum (log2 units) of a row; sums of this lane's P (fp32, bf16)
+};
+
+__device__ __forceinline__ float group_max(float x) {   // over the four lane groups
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+}
+
+__device__ __forceinline__ bf16x8 v_operand16(const uint16_t* v, int vlane, int dt) {
+  const uint16_t* p = v + vlane + 16 * dt;
+  const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p));
+  const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p + 16 * TV));
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Scores of the block (s[n][half]: keys 16 half + 4 q + i) and the staged V
+// against the wave's rows; bit k of seen[n]: this lane's row sees key k.
+template <int RN>
+__device__ __forceinline__ void attend_few(FewRows<RN>& r, f32x4 (&s)[RN][2], const uint16_t* v,
+                                           const uint32_t (&seen)[RN], float sc, int q, int vlane) {
+  bf16x8 p[RN];
+#pragma unroll
+  for (int n = 0; n < RN; ++n) {
+    if (__any(seen[n] != 0xffffffffu)) {
+      const uint32_t mine = seen[n] >> (4 * q);
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        if (!(mine >> (16 * (x >> 2) + (x & 3)) & 1)) s[n][x >> 2][x & 3] = -INFINITY;
+    }
+    float mx = s[n][0][0];
+#pragma unroll
+    for (int x = 1; x < 8; ++x) mx = fmaxf(mx, s[n][x >> 2][x & 3]);
+    mx = group_max(mx) * sc;                 // sc > 0
+    if (__any(mx > r.m[n] + SLACK)) {
+      const float m = fmaxf(r.m[n], mx), alpha = r.m[n] == m ? 1.0f : fast_exp2(r.m[n] - m);
+      r.m[n] = m;
+      r.l[n] *= alpha;
+      r.lo[n] *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) r.o[n][dt][x] *= alpha;
+    }
+    const float base = r.m[n] == -INFINITY ? 0.0f : r.m[n];   // nothing seen yet: every P is 2^-inf = 0
+    const bf16e2 one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const float e = fast_exp2(fmaf(s[n][x >> 2][x & 3], sc, -base));
+      r.l[n] += e;
+      p[n][x] = (__bf16)e;                   // rounded for the product; O is divided by the sum of these
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      r.lo[n] = __builtin_amdgcn_fdot2_f32_bf16(bf16e2{p[n][2 * x], p[n][2 * x + 1]}, one, r.lo[n], false);
+  }
+#pragma unroll
+  for (int dt = 0; dt < 8; ++dt) {
+    const bf16x8 av = v_operand16(v, vlane, dt);
+#pragma unroll
+    for (int n = 0; n < RN; ++n) r.o[n][dt] = mfma16(av, p[n], r.o[n][dt]);
+  }
+}
+
+// Infinities and NaN in the V of drafted keys, as in add_not_finite.
+template <int RN>
+__device__ __forceinline__ void add_not_finite_few(FewRows<RN>& r, uint16_t* flags, const uint16_t* v, int64_t ss,
+                                                   int n, const uint32_t (&seen)[RN], int q, int vlane, int lane) {
+  bf16x8 sees[RN];
+#pragma unroll
+  for (int t = 0; t < RN; ++t)
+#pragma unroll
+    for (int x = 0; x < 8; ++x) sees[t][x] = (__bf16)((seen[t] >> (16 * (x >> 2) + 4 * q + (x & 3)) & 1) ? 1.0f : 0.0f);
+  for (int what = 0; what < 3; ++what) {
+    flag_not_finite(flags, v, ss, n, what, lane);
+    wave_fence();
+    const float add = what == 2 ? __uint_as_float(0x7fc00000u) : what ? -INFINITY : INFINITY;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+      const bf16x8 av = v_operand16(flags, vlane, dt);
+#pragma unroll
+      for (int t = 0; t < RN; ++t) {
+        f32x4 c = {};
+        c = mfma16(av, sees[t], c);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) r.o[t][dt][x] += c[x] > 0.0f ? add : 0.0f;
+      }
+    }
+    wave_fence();
+  }
+}
+
+template <int TYPE, int RN>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3 : 2))) void k_tree_few(TreeArgs a) {
+  constexpr int ROWS = 16 * RN;
+  // V blocks of the four waves; at the end their O, a tile of 16 rows at a time
+  __shared__ __align__(16) uint16_t vs[4 * KB * TV];
+  static_assert(sizeof(vs) >= 4 * 16 * OP * sizeof(float), "the join buffer lies in the V blocks");
   __shared__ float ml[4][ROWS][4];
   __shared__ int64_t sh64[4];
   __shared__ int sh[8];
@@ -342,145 +444,158 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   if (!find_item<ROWS, 256>(a, blockIdx.x, it, sh64, sh)) return;
   const Seq sq = sequence(a, it.b);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int c = lane & 31, h = lane >> 5;
-  WaveTile& t = tiles[wave];
-  // transpose-read source of this lane inside a staged V block: in each
-  // 16-lane group, output lane i, element e is element i % 4 of the 8 bytes
-  // addressed by lane 4 e + i / 4
-  const int grp = lane >> 4, li = lane & 15;
-  const int vlane = (4 * (grp >> 1) + (li >> 2)) * TV + 16 * (grp & 1) + 4 * (li & 3);
+  const int c = lane & 15, q = lane >> 4;
+  uint16_t* const v = vs + wave * KB * TV;
+  // transpose-read source of this lane in a staged V block: in each 16-lane
+  // group, output lane i, element e is element i % 4 of the 8 bytes addressed
+  // by lane 4 e + i / 4
+  const int vlane = (4 * q + (c >> 2)) * TV + 4 * (c & 3);
 
-  Rows r;
-  const int row = it.tile * ROWS + c, tok = row / a.g;
-  const bool live = tok < sq.T;
-  {
-    const uint16_t* q = (const uint16_t*)a.q.p + (int64_t)(sq.row0 + (live ? tok : 0)) * a.q.ss +
-                        (int64_t)(it.head * a.g + (live ? row - tok * a.g : 0)) * a.q.sh + h * 64;
+  FewRows<RN> r;
+  int tok[RN];
 #pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      const bf16x8 y = load16(q + 8 * x);
-      r.q[x] = live ? y : zero8();
+  for (int n = 0; n < RN; ++n) {
+    const int row = it.tile * ROWS + 16 * n + c;
+    tok[n] = row / a.g;
+    const bool live = tok[n] < sq.T;
+    const uint16_t* qp = (const uint16_t*)a.q.p + (int64_t)(sq.row0 + (live ? tok[n] : 0)) * a.q.ss +
+                         (int64_t)(it.head * a.g + (live ? row - tok[n] * a.g : 0)) * a.q.sh;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const bf16x8 y = load16(qp + channel<TYPE>(x, q));
+      r.q[n][x] = live ? y : zero8();
     }
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) r.o[n][dt] = f32x4{};
+    r.m[n] = -INFINITY;
+    r.l[n] = r.lo[n] = 0.0f;
   }
-#pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-    for (int x = 0; x < 16; ++x) r.o[dt][x] = 0.0f;
-  r.m = -INFINITY;
-  r.l = r.lo = 0.0f;
 
   const int32_t* pages = a.pages + (int64_t)it.b * a.max_pages;
-  Raw<TYPE> raw;
+  Raw32<TYPE> raw;
   int t0 = it.c0 + KB * wave;
   if (t0 < it.c1) load_block<TYPE>(raw, a, pages, it.head, t0, it.c1, lane);
   for (; t0 < it.c1; t0 += 4 * KB) {
-    const uint32_t seen = raw.seen;
-    stage_block<TYPE>(t, raw, lane);
+    uint32_t seen[RN];
+#pragma unroll
+    for (int n = 0; n < RN; ++n) seen[n] = raw.seen;
+    stage_v<TYPE>(v, raw, lane);
+    f32x4 s[RN][2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      bf16x8 op[4];
+      k_operands<TYPE>(op, raw, half, q);
+#pragma unroll
+      for (int n = 0; n < RN; ++n) {
+        s[n][half] = f32x4{};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[n][half] = mfma16(op[x], r.q[n][x], s[n][half]);
+      }
+    }
     if (t0 + 4 * KB < it.c1) load_block<TYPE>(raw, a, pages, it.head, t0 + 4 * KB, it.c1, lane);
     wave_fence();
-    attend(r, t, seen, a.sc, c, h, vlane);
+    attend_few<RN>(r, s, v, seen, a.sc, q, vlane);
     wave_fence();
   }
   if (it.chunk == it.chunks - 1) {
     const uint16_t* kb = (const uint16_t*)a.k.p + (int64_t)sq.row0 * a.k.ss + (int64_t)it.head * a.k.sh;
     const uint16_t* vb = (const uint16_t*)a.v.p + (int64_t)sq.row0 * a.v.ss + (int64_t)it.head * a.v.sh;
     for (int d0 = KB * wave; d0 < sq.T; d0 += 4 * KB) {
-      u32x4 kr[8], vr[8];
       uint64_t odd = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int d = min(d0 + 4 * i + lane / 16, sq.T - 1);
-        kr[i] = *reinterpret_cast<const u32x4*>(kb + (int64_t)d * a.k.ss + lane % 16 * 8);
-        vr[i] = *reinterpret_cast<const u32x4*>(vb + (int64_t)d * a.v.ss + lane % 16 * 8);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
         const int key = 4 * i + lane / 16;
+        const u32x4 raw_v = *reinterpret_cast<const u32x4*>(vb + (int64_t)min(d0 + key, sq.T - 1) * a.v.ss + lane % 16 * 8);
         u32x4 keep;
-        odd |= __ballot(not_finite(vr[i], keep));
         const u32x4 none = {};
-        *reinterpret_cast<u32x4*>(&t.k[key * TK + lane % 16 * 8]) = kr[i];
-        *reinterpret_cast<u32x4*>(&t.v[key * TV + lane % 16 * 8]) = d0 + key < sq.T ? keep : none;
+        odd |= __ballot(not_finite(raw_v, keep));
+        *reinterpret_cast<u32x4*>(v + key * TV + lane % 16 * 8) = d0 + key < sq.T ? keep : none;
       }
-      uint32_t seen = sq.T - d0 >= KB ? 0xffffffffu : (1u << (sq.T - d0)) - 1;
-      if (a.mask) {
-        const uint32_t* mr = a.mask + (int64_t)(sq.row0 + min(tok, sq.T - 1)) * (2 * a.mask_words);
-        seen &= mr[d0 >> 5];
-      } else {
-        const int n = tok + 1 - d0;        // keys d0 .. tok
-        seen &= n >= KB ? 0xffffffffu : n > 0 ? (1u << n) - 1 : 0u;
+      f32x4 s[RN][2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const uint16_t* kp = kb + (int64_t)min(d0 + 16 * half + c, sq.T - 1) * a.k.ss;
+#pragma unroll
+        for (int n = 0; n < RN; ++n) s[n][half] = f32x4{};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const bf16x8 op = load16(kp + channel<TYPE>(x, q));
+#pragma unroll
+          for (int n = 0; n < RN; ++n) s[n][half] = mfma16(op, r.q[n][x], s[n][half]);
+        }
       }
+      uint32_t seen[RN];
+#pragma unroll
+      for (int n = 0; n < RN; ++n) seen[n] = seen_drafts(a, sq, tok[n], d0);
       wave_fence();
-      attend(r, t, seen, a.sc, c, h, vlane);
+      attend_few<RN>(r, s, v, seen, a.sc, q, vlane);
       wave_fence();
-      if (odd) add_not_finite(r.o, t.v, vb + (int64_t)d0 * a.v.ss, a.v.ss, sq.T - d0, seen, h, vlane, lane);
+      if (odd) add_not_finite_few<RN>(r, v, vb + (int64_t)d0 * a.v.ss, a.v.ss, sq.T - d0, seen, q, vlane, lane);
     }
   }
 
   // the waves' parts of each row, weighed by their maxima
-  if (h == 0) {
-    ml[wave][c][0] = r.m;
-    ml[wave][c][1] = r.lo;
-    ml[wave][c][2] = r.l;
+#pragma unroll
+  for (int n = 0; n < RN; ++n) {
+    r.l[n] += __shfl_xor(r.l[n], 16);
+    r.l[n] += __shfl_xor(r.l[n], 32);
+    r.lo[n] += __shfl_xor(r.lo[n], 16);
+    r.lo[n] += __shfl_xor(r.lo[n], 32);
+    if (q == 0) *reinterpret_cast<float4*>(ml[wave][16 * n + c]) = make_float4(r.m[n], r.lo[n], r.l[n], 0.0f);
   }
-  __syncthreads();                         // also: the staged blocks are done with
-  float* buf = reinterpret_cast<float*>(tiles) + wave * ROWS * OP;
-  static_assert(sizeof(tiles) >= 4 * ROWS * OP * sizeof(float), "the join buffer lies in the tiles");
-  {
-    float m = ml[0][c][0];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) m = fmaxf(m, ml[w][c][0]);
-    const float f = r.m == -INFINITY ? 0.0f : fast_exp2(r.m - m);
+  for (int n = 0; n < RN; ++n) {
+    __syncthreads();                       // the staged blocks, or the tile before, are done with
+    float* buf = reinterpret_cast<float*>(vs) + wave * 16 * OP;
+    {
+      float m = ml[0][16 * n + c][0];
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
+      for (int w = 1; w < 4; ++w) m = fmaxf(m, ml[w][16 * n + c][0]);
+      const float f = r.m[n] == -INFINITY ? 0.0f : fast_exp2(r.m[n] - m);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(buf + c * OP + 32 * dt + 8 * i + 4 * h) =
-            make_float4(r.o[dt][4 * i] * f, r.o[dt][4 * i + 1] * f, r.o[dt][4 * i + 2] * f, r.o[dt][4 * i + 3] * f);
-  }
-  __syncthreads();
-  const int jr = tid >> 3, part = tid & 7;               // row of the tile, 16 channels
-  const int jrow = it.tile * ROWS + jr, jtok = jrow / a.g;
-  if (jtok >= sq.T) return;
-  float m = ml[0][jr][0];
-#pragma unroll
-  for (int w = 1; w < 4; ++w) m = fmaxf(m, ml[w][jr][0]);
-  float l = 0.0f, lo = 0.0f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float f = ml[w][jr][0] == -INFINITY ? 0.0f : fast_exp2(ml[w][jr][0] - m);
-    lo += ml[w][jr][1] * f;
-    l += ml[w][jr][2] * f;
-  }
-  float o[16];
-#pragma unroll
-  for (int x = 0; x < 16; ++x) o[x] = 0.0f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(tiles) + (w * ROWS + jr) * OP +
-                                                        part * 16 + 4 * x);
-      o[4 * x] += y.x; o[4 * x + 1] += y.y; o[4 * x + 2] += y.z; o[4 * x + 3] += y.w;
+      for (int dt = 0; dt < 8; ++dt)
+        *reinterpret_cast<float4*>(buf + c * OP + 16 * dt + 4 * q) =
+            make_float4(r.o[n][dt][0] * f, r.o[n][dt][1] * f, r.o[n][dt][2] * f, r.o[n][dt][3] * f);
     }
-  if (it.chunks == 1) {
-    const float inv = lo > 0.0f ? 1.0f / lo : lo == 0.0f ? 0.0f : lo;   // no key seen: 0; NaN stays
-    const int head = it.head * a.g + jrow - jtok * a.g;
-    uint16_t* to = a.o + (int64_t)(sq.row0 + jtok) * a.o_ss + (int64_t)head * a.o_sh + part * 16;
-    bf16x8 y[2];
+    __syncthreads();
+    const int jr = tid >> 4, part = tid & 15;              // row of the tile, 8 channels
+    const int row = it.tile * ROWS + 16 * n + jr, jtok = row / a.g;
+    if (jtok >= sq.T) continue;
+    const float (*mr)[ROWS][4] = ml;
+    float m = mr[0][16 * n + jr][0];
 #pragma unroll
-    for (int x = 0; x < 16; ++x) y[x >> 3][x & 7] = (__bf16)(o[x] * inv);
-    *reinterpret_cast<bf16x8*>(to) = y[0];
-    *reinterpret_cast<bf16x8*>(to + 8) = y[1];
-    if (a.lse && part == 0)
-      a.lse[(int64_t)head * a.n_rows + sq.row0 + jtok] = l == 0.0f ? -INFINITY : (m + fast_log2(l)) * LN2;
-  } else {
-    const int64_t at = (int64_t)blockIdx.x * ROWS + jr;
-    float* to = a.part_o + at * D + part * 16;
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, mr[w][16 * n + jr][0]);
+    float l = 0.0f, lo = 0.0f, o[8];
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-      *reinterpret_cast<float4*>(to + 4 * x) = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
-    if (part == 0) *reinterpret_cast<float4*>(a.part_ml + at * 4) = make_float4(m, lo, l, 0.0f);
+    for (int x = 0; x < 8; ++x) o[x] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float wm = mr[w][16 * n + jr][0], f = wm == -INFINITY ? 0.0f : fast_exp2(wm - m);
+      lo += mr[w][16 * n + jr][1] * f;
+      l += mr[w][16 * n + jr][2] * f;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(vs) + (w * 16 + jr) * OP +
+                                                          part * 8 + 4 * x);
+        o[4 * x] += y.x; o[4 * x + 1] += y.y; o[4 * x + 2] += y.z; o[4 * x + 3] += y.w;
+      }
+    }
+    if (it.chunks == 1) {
+      const float inv = lo > 0.0f ? 1.0f / lo : lo == 0.0f ? 0.0f : lo;   // no key seen: 0; NaN stays
+      const int head = it.head * a.g + row - jtok * a.g;
+      bf16x8 y;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) y[x] = (__bf16)(o[x] * inv);
+      *reinterpret_cast<bf16x8*>(a.o + (int64_t)(sq.row0 + jtok) * a.o_ss + (int64_t)head * a.o_sh + part * 8) = y;
+      if (a.lse && part == 0)
+        a.lse[(int64_t)head * a.n_rows + sq.row0 + jtok] = l == 0.0f ? -INFINITY : (m + fast_log2(l)) * LN2;
+    } else {
+      const int64_t at = (int64_t)blockIdx.x * ROWS + 16 * n + jr;
+      float* to = a.part_o + at * D + part * 8;
+      *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<float4*>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
+      if (part == 0) *reinterpret_cast<float4*>(a.part_ml + at * 4) = make_float4(m, lo, l, 0.0f);
+    }
   }
 }
 
@@ -585,8 +700,6 @@ __device__ __forceinline__ void mask_unit(f32x16& s, uint32_t seen, int h) {
     if (!(mine >> (8 * (x >> 2) + (x & 3)) & 1)) s[x] = -INFINITY;
 }
 
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16e2;
-
 // The softmax of a unit in pieces that fit between MFMAs: 0, 1 maxima of 8
 // scores, 2 the running maximum, 3-18 one exponential each, 19, 20 packing
 // and the sum of the packed, 21 the sums.
@@ -623,8 +736,8 @@ __device__ __forceinline__ void soft_piece(int piece, f32x16& s, float sc, Rows&
     for (int x = 0; x < 4; ++x)
       z.ro = __builtin_amdgcn_fdot2_f32_bf16(bf16e2{p[half][2 * x], p[half][2 * x + 1]}, one, z.ro, false);
   } else {
-    if (WL) r.l = r.l * z.alpha + half_sum(z.rs);
-    r.lo = r.lo * z.alpha + half_sum(z.ro);
+    if (WL) r.l = r.l * z.alpha + z.rs;
+    r.lo = r.lo * z.alpha + z.ro;
   }
 }
 
@@ -811,13 +924,7 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
       for (int sub = wk; sub < 2; sub += WK) {
         const int k0 = d0 + 32 * sub;
         if (!active || k0 >= sq.T) continue;
-        uint32_t seen = sq.T - k0 >= 32 ? 0xffffffffu : (1u << (sq.T - k0)) - 1;
-        if (a.mask) {
-          seen &= a.mask[(int64_t)(sq.row0 + min(tok, sq.T - 1)) * (2 * a.mask_words) + (k0 >> 5)];
-        } else {
-          const int n = tok + 1 - k0;                      // keys k0 .. tok
-          seen &= n >= 32 ? 0xffffffffu : n > 0 ? (1u << n) - 1 : 0u;
-        }
+        const uint32_t seen = seen_drafts(a, sq, tok, k0);
         unit_alone(r, seen, a.sc, h, st[0].k + klane + 32 * sub * TK, st[0].v + vlane + 32 * sub * TV);
         if (odd) {                                         // flags in a place of the wave's own
           uint16_t* own = st[1].k + wave * (KB * TV);
@@ -829,6 +936,8 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
     }
   }
 
+  r.l = half_sum(r.l);
+  r.lo = half_sum(r.lo);
   if constexpr (WK == 2) {                                 // the second key group's part joins the first's
     float* buf = reinterpret_cast<float*>(st) + wr * (32 * OP + 128);
     static_assert(sizeof(st) >= WR * (32 * OP + 128) * sizeof(float), "the join buffer lies in the stages");
@@ -953,11 +1062,12 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
 TreeShape tree_shape(const mmi_tree& t, int Hkv, int cus) {
   TreeShape s{};
   const int g = t.Hq / Hkv;
-  // up to 64 rows a head the cache's bytes bound the work (below); the wide
-  // tiles hold a compute unit each, two narrow ones share one
+  // what bounds the work changes at 32 rows a head (16 rows: half the softmax
+  // and products of 32); a wide workgroup holds a compute unit, three or two
+  // of the few-row ones share it
   const int rows = t.max_rows * g;
-  s.rows = rows <= 64 ? 32 : rows <= 128 ? 128 : 256;
-  s.target = s.rows == 32 ? 2 * cus : cus;
+  s.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
+  s.target = cus * (s.rows == 16 ? 3 : s.rows == 32 ? 2 : 1);
   // tiles of all sequences, and `target` chunks more (each sequence's last chunk may be short)
   const int64_t most = (t.max_rows * (int64_t)g + s.rows - 1) / s.rows;
   const int64_t tiles = std::min<int64_t>(most * t.n_seq, ((int64_t)t.n_rows * g + (int64_t)t.n_seq * (s.rows - 1)) / s.rows);
@@ -976,7 +1086,8 @@ TreeShape tree_shape(const mmi_tree& t, int Hkv, int cus) {
 template <int TYPE>
 static void launch_type(const TreeArgs& a, int rows, hipStream_t st) {
   const dim3 grid((unsigned)a.items);
-  if (rows == 32) hipLaunchKernelGGL(k_tree<TYPE>, grid, dim3(256), 0, st, a);
+  if (rows == 16) hipLaunchKernelGGL((k_tree_few<TYPE, 1>), grid, dim3(256), 0, st, a);
+  else if (rows == 32) hipLaunchKernelGGL((k_tree_few<TYPE, 2>), grid, dim3(256), 0, st, a);
   else if (rows == 128 && a.lse) hipLaunchKernelGGL((k_tree_wide<TYPE, 4, true>), grid, dim3(NTW), 0, st, a);
   else if (rows == 128) hipLaunchKernelGGL((k_tree_wide<TYPE, 4, false>), grid, dim3(NTW), 0, st, a);
   else if (a.lse) hipLaunchKernelGGL((k_tree_wide<TYPE, 8, true>), grid, dim3(NTW), 0, st, a);
@@ -995,7 +1106,8 @@ hipError_t launch_tree(const TreeArgs& a, int type, int rows, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.max_len <= CHUNK) return e;   // one chunk a sequence at most
   const dim3 join((unsigned)(a.max_rows * a.g * a.c.Hkv * a.n_seq));
-  if (rows == 32) hipLaunchKernelGGL(k_tree_join<32>, join, dim3(256), 0, st, a);
+  if (rows == 16) hipLaunchKernelGGL(k_tree_join<16>, join, dim3(256), 0, st, a);
+  else if (rows == 32) hipLaunchKernelGGL(k_tree_join<32>, join, dim3(256), 0, st, a);
   else if (rows == 128) hipLaunchKernelGGL(k_tree_join<128>, join, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(k_tree_join<256>, join, dim3(256), 0, st, a);
   return hipGetLastError();
