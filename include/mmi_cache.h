@@ -143,7 +143,7 @@ typedef struct mmi_tree {
 } mmi_tree;
 
 /* Bytes of device workspace that a batch of these bounds needs; it depends on
- * the integers of `tree` and the cache's Hkv only. MMI_ERR_UNSUPPORTED for
+ * the integers of `tree` and the cache's type and Hkv only. MMI_ERR_UNSUPPORTED for
  * bounds that ask for more than 2^22 workgroups. */
 int mmi_tree_workspace(mmi_ctx* ctx, const mmi_cache* cache, const mmi_tree* tree, size_t* bytes);
 

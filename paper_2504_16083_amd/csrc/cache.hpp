@@ -64,7 +64,7 @@ struct TreeShape {                 // how a batch is cut, from its bounds alone
   int32_t target, items;
   size_t part_o, part_ml, rec, bytes;   // offsets into the workspace, and its size
 };
-TreeShape tree_shape(const mmi_tree& t, int Hkv, int cus);
+TreeShape tree_shape(const mmi_tree& t, int Hkv, int type, int cus);
 hipError_t launch_tree(const TreeArgs& a, int type, int rows, hipStream_t st);
 
 // ---------------------------------------------------------------- cache.hip

@@ -76,20 +76,48 @@ struct Item {
   int c0, c1;                                // cached tokens
 };
 
+// Items of the batch with chunks of this length.
+template <int ROWS, int NT>
+__device__ __forceinline__ int64_t count_items(const TreeArgs& a, int chunk, int64_t* sh64) {
+  int64_t n = 0, before;
+  for (int b = threadIdx.x; b < a.n_seq; b += NT) {
+    const Seq s = sequence(a, b);
+    n += (int64_t)((s.T * a.g + ROWS - 1) / ROWS) * max(1, (s.L + chunk - 1) / chunk);
+  }
+  return block_scan<NT>(n, &before, sh64) * a.c.Hkv;
+}
+
 // Item `it` of the batch. The chunk length follows from the work of the whole
 // batch (cached tokens x tiles x heads, cut into `target` parts), so long
-// sequences get many chunks and short ones few, whatever the bounds were.
+// sequences get many chunks and short ones few, whatever the bounds were. The
+// last chunks are shorter than the others, so that there are more items than
+// parts; as `target` of them run at once, the chunks are then made longer
+// until all start together (a second round of a few items takes as long as
+// the first: a ragged batch of 32 decoded tokens took 74 us for 65).
 template <int ROWS, int NT>
 __device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, int64_t* sh64, int* sh) {
   const int tid = threadIdx.x;
-  int64_t work = 0, before;
+  int64_t work = 0, units = 0, before;
   for (int b = tid; b < a.n_seq; b += NT) {
     const Seq s = sequence(a, b);
-    work += (int64_t)((s.T * a.g + ROWS - 1) / ROWS) * s.L;
+    const int tiles = (s.T * a.g + ROWS - 1) / ROWS;
+    work += (int64_t)tiles * s.L;
+    units += tiles;
   }
   work = block_scan<NT>(work, &before, sh64) * a.c.Hkv;
-  const int64_t len = (work + a.target - 1) / a.target;
-  const int chunk = (int)((max(len, (int64_t)1) + CHUNK - 1) / CHUNK * CHUNK);
+  auto chunk_of = [&](int64_t parts) -> int {
+    const int64_t len = (work + parts - 1) / parts;
+    return (int)((max(len, (int64_t)1) + CHUNK - 1) / CHUNK * CHUNK);
+  };
+  int chunk = chunk_of(a.target);
+  int64_t items = count_items<ROWS, NT>(a, chunk, sh64);
+  if (items > a.target) {
+    units = block_scan<NT>(units, &before, sh64) * a.c.Hkv;
+    if (units < a.target) {        // at most units + work / chunk items: the second length always fits
+      const int longer = chunk_of(max((int64_t)1, a.target * a.target / items)), safe = chunk_of(a.target - units);
+      chunk = longer < safe && count_items<ROWS, NT>(a, longer, sh64) <= a.target ? longer : safe;
+    }
+  }
   if (tid == 0) sh[0] = -1;
   int64_t base = 0;
   for (int b0 = 0; b0 < a.n_seq; b0 += NT) {
@@ -1059,15 +1087,17 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
     a.lse[(int64_t)qh * a.n_rows + sq.row0 + tok] = l == 0.0f ? -INFINITY : (m + fast_log2(l)) * LN2;
 }
 
-TreeShape tree_shape(const mmi_tree& t, int Hkv, int cus) {
+TreeShape tree_shape(const mmi_tree& t, int Hkv, int type, int cus) {
   TreeShape s{};
   const int g = t.Hq / Hkv;
   // what bounds the work changes at 32 rows a head (16 rows: half the softmax
   // and products of 32); a wide workgroup holds a compute unit, three or two
-  // of the few-row ones share it
+  // of the few-row ones share it. Two of them read 16-bit rows faster than
+  // three (32 sequences of 8192 tokens and 8 heads: 192 us for 223), three
+  // the smaller rows (E4M3 121 us for 137, E2M1 69 for 84).
   const int rows = t.max_rows * g;
   s.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
-  s.target = cus * (s.rows == 16 ? 3 : s.rows == 32 ? 2 : 1);
+  s.target = cus * (s.rows > 32 ? 1 : s.rows == 32 || type == MMI_CACHE_BF16 ? 2 : 3);
   // tiles of all sequences, and `target` chunks more (each sequence's last chunk may be short)
   const int64_t most = (t.max_rows * (int64_t)g + s.rows - 1) / s.rows;
   const int64_t tiles = std::min<int64_t>(most * t.n_seq, ((int64_t)t.n_rows * g + (int64_t)t.n_seq * (s.rows - 1)) / s.rows);

@@ -1657,7 +1657,7 @@ int mmi_tree_workspace(mmi_ctx* ctx, const mmi_cache* cache, const mmi_tree* tre
     cache_dev(cache);
     const mmi_tree t = tree_checked(cache, tree);
     if (!ctx || !bytes) fail(MMI_ERR_INVALID_ARG, "ctx/bytes is NULL");
-    *bytes = tree_shape(t, cache->Hkv, ctx->cus).bytes;
+    *bytes = tree_shape(t, cache->Hkv, cache->type, ctx->cus).bytes;
   });
 }
 
@@ -1668,7 +1668,7 @@ int mmi_tree_attention(mmi_ctx* ctx, const mmi_cache* cache, const mmi_tree* tre
     const mmi_tree t = tree_checked(cache, tree);
     TreeArgs a = tree_args(cache, t, q, k, v, o, lse);
     if (!ctx) fail(MMI_ERR_INVALID_ARG, "ctx is NULL");
-    const TreeShape s = tree_shape(t, cache->Hkv, ctx->cus);
+    const TreeShape s = tree_shape(t, cache->Hkv, cache->type, ctx->cus);
     if (!workspace || (uintptr_t)workspace % 16) fail(MMI_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
     if (workspace_bytes < s.bytes)
       fail(MMI_ERR_INVALID_ARG, "workspace of %zu bytes, %zu needed", workspace_bytes, s.bytes);
