@@ -653,68 +653,79 @@ template <int TYPE>
 struct Raw64 {                         // a thread's pieces of a stage: piece i is number tid + i * NTW
   static constexpr int CPR = Codec<TYPE>::ROW / 16;        // pieces a row
   static constexpr int N = SK * CPR / NTW > 0 ? SK * CPR / NTW : 1;
-  static constexpr int LIVE = SK * CPR < NTW ? SK * CPR : NTW;   // threads with pieces
+  static constexpr int LIVE = SK * CPR < NTW ? SK * CPR / 64 : NTW / 64;   // waves with pieces
   u32x4 k[N], v[N];
   uint32_t ks[N], vs[N];
-  int ok[N];
 };
 
+// Where a wave's pieces come from. Its 64 pieces i are 4, 8 or 16 whole rows,
+// which lie in one page and follow each other: one page number and scalar base
+// a load, and a lane's offset that never changes.
 struct KeySource {
   const int32_t* pages;
-  int head, c1, tid;
+  int head, c0, c1, wave, lane;
+  int zero;                            // in a vector register: keeps the page table's loads vector loads
 };
 
 template <int TYPE>
-__device__ __forceinline__ int key_of(int tid, int i) { return (tid % Raw64<TYPE>::LIVE + i * NTW) / Raw64<TYPE>::CPR; }
+__device__ __forceinline__ int first_key(int wave, int i) {
+  return (wave % Raw64<TYPE>::LIVE * 64 + i * NTW) / Raw64<TYPE>::CPR;
+}
 
+// The numbers stay in a vector register until they are used, a stage later: a
+// scalar load would share its counter with the LDS reads of the slots between.
 template <int TYPE>
 __device__ __forceinline__ void page_ids(int (&p)[Raw64<TYPE>::N], const TreeArgs& a, const KeySource& s, int t0) {
 #pragma unroll
   for (int i = 0; i < Raw64<TYPE>::N; ++i)
-    p[i] = s.pages[min(t0 + key_of<TYPE>(s.tid, i), s.c1 - 1) >> a.c.shift];
+    p[i] = s.pages[(min(t0 + first_key<TYPE>(s.wave, i), s.c1 - 1) >> a.c.shift) + s.zero];
 }
 
+// Pages outside the cache are read as page 0, which is there; their keys are
+// masked, and their V staged as zero.
 template <int TYPE>
 __device__ __forceinline__ void load_stage(Raw64<TYPE>& r, const int (&p)[Raw64<TYPE>::N], const TreeArgs& a,
                                            const KeySource& s, int t0) {
   typedef Raw64<TYPE> R;
+  if (R::LIVE < NTW / 64 && s.wave >= R::LIVE) return;
 #pragma unroll
   for (int i = 0; i < R::N; ++i) {
-    const int t = t0 + key_of<TYPE>(s.tid, i);
-    const bool there = (uint32_t)p[i] < (uint64_t)a.c.n_pages;
-    r.ok[i] = there && t < s.c1;
-    const int64_t page = there ? p[i] : 0;
+    const int t = t0 + first_key<TYPE>(s.wave, i);
+    const int id = __builtin_amdgcn_readfirstlane(p[i]);
+    const int64_t page = (uint32_t)id < (uint64_t)a.c.n_pages ? id : 0;
     const int in = (s.head << a.c.shift) + (t & ((1 << a.c.shift) - 1));
-    const int64_t at = page * a.c.page_stride + (int64_t)in * Codec<TYPE>::ROW + s.tid % R::CPR * 16;
-    r.k[i] = *reinterpret_cast<const u32x4*>(a.c.k + at);
-    r.v[i] = *reinterpret_cast<const u32x4*>(a.c.v + at);
+    const int64_t at = page * a.c.page_stride + (int64_t)in * Codec<TYPE>::ROW;
+    r.k[i] = reinterpret_cast<const u32x4*>(a.c.k + at)[s.lane];
+    r.v[i] = reinterpret_cast<const u32x4*>(a.c.v + at)[s.lane];
     if constexpr (Codec<TYPE>::SCALED) {
       const int64_t sat = page * a.c.scale_stride + (int64_t)in * 4;
-      r.ks[i] = *reinterpret_cast<const uint32_t*>((const uint8_t*)a.c.ks + sat);
-      r.vs[i] = *reinterpret_cast<const uint32_t*>((const uint8_t*)a.c.vs + sat);
+      r.ks[i] = reinterpret_cast<const uint32_t*>((const uint8_t*)a.c.ks + sat)[s.lane / R::CPR];
+      r.vs[i] = reinterpret_cast<const uint32_t*>((const uint8_t*)a.c.vs + sat)[s.lane / R::CPR];
     }
   }
 }
 
+// `there`: the stage's keys that exist; the others weigh nothing, whatever
+// their places hold.
 template <int TYPE>
-__device__ __forceinline__ void write_stage(Stage64& st, const Raw64<TYPE>& r, int tid) {
+__device__ __forceinline__ void write_stage(Stage64& st, const Raw64<TYPE>& r, int wave, int lane, uint64_t there) {
   typedef Raw64<TYPE> R;
-  if (R::LIVE < NTW && tid >= R::LIVE) return;
+  if (R::LIVE < NTW / 64 && wave >= R::LIVE) return;
 #pragma unroll
   for (int i = 0; i < R::N; ++i) {
-    const int key = key_of<TYPE>(tid, i), piece = tid % R::CPR;
-    const u32x4 none = {};
+    const int key = first_key<TYPE>(wave, i) + lane / R::CPR, piece = lane % R::CPR;
     put_piece<TYPE>(&st.k[key * TK], r.k[i], r.ks[i], piece);
-    // a key that does not exist weighs nothing, whatever its place in the page holds
-    put_piece<TYPE>(&st.v[key * TV], r.ok[i] ? r.v[i] : none, r.ok[i] ? r.vs[i] : 0u, piece);
+    u32x4 v = r.v[i];
+    if (there != ~0ull && !(there >> key & 1)) v = u32x4{};
+    put_piece<TYPE>(&st.v[key * TV], v, there != ~0ull && !(there >> key & 1) ? 0u : r.vs[i], piece);
   }
 }
 
-// MFMA operand i of a slot: even ones K rows of the next unit, odd ones
+// MFMA operand i of a slot: first the K rows of the next unit, then the
 // transposed V of the last.
 __device__ __forceinline__ bf16x8 slot_operand(int i, const uint16_t* kp, const uint16_t* vp) {
-  const int x = i >> 1;
-  if ((i & 1) == 0) return *reinterpret_cast<const bf16x8*>(kp + x * 8);
+  const int x = i & 7;
+  if (i < 8) return *reinterpret_cast<const bf16x8*>(kp + x * 8);
   const uint16_t* p = vp + 16 * (x >> 2) * TV + 32 * (x & 3);
   const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p));
   const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4*)(p + 8 * TV));
@@ -727,6 +738,12 @@ __device__ __forceinline__ void mask_unit(f32x16& s, uint32_t seen, int h) {
   for (int x = 0; x < 16; ++x)
     if (!(mine >> (8 * (x >> 2) + (x & 3)) & 1)) s[x] = -INFINITY;
 }
+
+// A use that keeps the computation of x where it is written: nothing reads
+// much of a slot's results before the next slot, and the compiler would move
+// it there, in one lump behind the MFMAs that it is to run beside.
+template <typename T>
+__device__ __forceinline__ void pin(T& x) { asm volatile("" : "+v"(x)); }
 
 // The softmax of a unit in pieces that fit between MFMAs: 0, 1 maxima of 8
 // scores, 2 the running maximum, 3-18 one exponential each, 19, 20 packing
@@ -743,6 +760,7 @@ __device__ __forceinline__ void soft_piece(int piece, f32x16& s, float sc, Rows&
 #pragma unroll
     for (int x = 1; x < 8; ++x) mx = fmaxf(mx, s[8 * piece + x]);
     z.mx = piece == 0 ? mx : fmaxf(z.mx, mx);
+    pin(z.mx);
   } else if (piece == 2) {
     const float mx = half_max(z.mx) * sc;                  // sc > 0
     const bool move = __any(mx > r.m + SLACK);
@@ -751,10 +769,13 @@ __device__ __forceinline__ void soft_piece(int piece, f32x16& s, float sc, Rows&
     r.m = mn;
     z.base = mn == -INFINITY ? 0.0f : mn;                  // nothing seen yet: every P is 2^-inf = 0
     z.rs = z.ro = 0.0f;
+    pin(z.base);
   } else if (piece < 19) {
     const int x = piece - 3;
-    s[x] = fast_exp2(fmaf(s[x], sc, -z.base));
-    if (WL) z.rs += s[x];
+    float e = fast_exp2(fmaf(s[x], sc, -z.base));
+    pin(e);
+    s[x] = e;
+    if (WL) z.rs += e;
   } else if (piece < 21) {
     const int half = piece - 19;
     const bf16e2 one = {(__bf16)1.0f, (__bf16)1.0f};
@@ -763,6 +784,8 @@ __device__ __forceinline__ void soft_piece(int piece, f32x16& s, float sc, Rows&
 #pragma unroll
     for (int x = 0; x < 4; ++x)
       z.ro = __builtin_amdgcn_fdot2_f32_bf16(bf16e2{p[half][2 * x], p[half][2 * x + 1]}, one, z.ro, false);
+    pin(z.ro);
+    pin(p[half]);
   } else {
     if (WL) r.l = r.l * z.alpha + z.rs;
     r.lo = r.lo * z.alpha + z.ro;
@@ -776,23 +799,32 @@ __device__ __forceinline__ void rescale(Rows& r, float alpha) {
     for (int x = 0; x < 16; ++x) r.o[dt][x] *= alpha;
 }
 
-template <bool WL>
-__device__ __forceinline__ void slot(Rows& r, f32x16& s_sm, f32x16& s_qk, const bf16x8 (&p_pv)[2], bf16x8 (&p_sm)[2],
-                                     float sc, const uint16_t* kp, const uint16_t* vp) {
-  constexpr int AHEAD = 3;
+constexpr int AHEAD = 3;
+
+// PRE: the first operands are there, read in the slot before; this one reads
+// the next one's (from kn, vn).
+template <bool WL, bool PRE>
+__device__ __forceinline__ void slot(Rows& r, bf16x8 (&op)[AHEAD + 1], f32x16& s_sm, f32x16& s_qk,
+                                     const bf16x8 (&p_pv)[2], bf16x8 (&p_sm)[2], float sc, const uint16_t* kp,
+                                     const uint16_t* vp, const uint16_t* kn, const uint16_t* vn) {
   SoftState z;
   const f32x16 zero = {};
-  bf16x8 op[AHEAD + 1];
+  if (!PRE) {
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) op[i] = slot_operand(i, kp, vp);
+    for (int i = 0; i < AHEAD; ++i) op[i] = slot_operand(i, kp, vp);
+  }
   int pc = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    if (i + AHEAD < 16) op[(i + AHEAD) % (AHEAD + 1)] = slot_operand(i + AHEAD, kp, vp);
+    const int j = i + AHEAD;
+    if (j < 16) op[j % (AHEAD + 1)] = slot_operand(j, kp, vp);
+    else if (PRE) op[j % (AHEAD + 1)] = slot_operand(j - 16, kn, vn);
     const bf16x8 av = op[i % (AHEAD + 1)];
-    const int x = i >> 1;
-    if ((i & 1) == 0) s_qk = mfma32(av, r.q[x], x == 0 ? zero : s_qk);
-    else r.o[x & 3] = mfma32(av, p_pv[x >> 2], r.o[x & 3]);
+    const int x = i & 7;
+    if (i < 8) {
+      s_qk = mfma32(av, r.q[x], x == 0 ? zero : s_qk);
+      pin(s_qk);
+    } else r.o[x & 3] = mfma32(av, p_pv[x >> 2], r.o[x & 3]);
     const int end = (i + 1) * PIECES / 16;
 #pragma unroll
     for (; pc < end; ++pc) soft_piece<WL>(pc, s_sm, sc, r, p_sm, z);
@@ -806,7 +838,7 @@ __device__ __forceinline__ void unit_alone(Rows& r, uint32_t seen, float sc, int
                                            const uint16_t* vp) {
   f32x16 s = {};
 #pragma unroll
-  for (int x = 0; x < 8; ++x) s = mfma32(slot_operand(2 * x, kp, vp), r.q[x], s);
+  for (int x = 0; x < 8; ++x) s = mfma32(slot_operand(x, kp, vp), r.q[x], s);
   mask_unit(s, seen, h);
   SoftState z;
   bf16x8 p[2];
@@ -814,7 +846,7 @@ __device__ __forceinline__ void unit_alone(Rows& r, uint32_t seen, float sc, int
   for (int pc = 0; pc < PIECES; ++pc) soft_piece<true>(pc, s, sc, r, p, z);
   rescale(r, z.alpha);
 #pragma unroll
-  for (int x = 0; x < 8; ++x) r.o[x & 3] = mfma32(slot_operand(2 * x + 1, kp, vp), p[x >> 2], r.o[x & 3]);
+  for (int x = 0; x < 8; ++x) r.o[x & 3] = mfma32(slot_operand(8 + x, kp, vp), p[x >> 2], r.o[x & 3]);
 }
 
 template <int TYPE, int WR, bool WL>
@@ -858,29 +890,37 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
   // stages, an even number of units a wave: what lies behind c1 is staged as nothing
   const int steps = (it.c1 - it.c0 + SK * WK - 1) / (SK * WK) * WK;
   if (steps > 0) {
-    const KeySource src = {a.pages + (int64_t)it.b * a.max_pages, it.head, it.c1, tid};
+    int zero = 0;
+    asm("" : "+v"(zero));
+    const KeySource src = {a.pages + (int64_t)it.b * a.max_pages, it.head, it.c0, it.c1, wave, lane, zero};
     // pages outside the cache are rare enough to ask once for the whole chunk
     int bad = 0;
     for (int p = (it.c0 >> a.c.shift) + tid; p <= (it.c1 - 1) >> a.c.shift; p += NTW)
       bad |= (uint32_t)src.pages[p] >= (uint64_t)a.c.n_pages;
     const bool any_bad = __syncthreads_or(bad);
-    auto seen_of = [&](int t0) -> uint32_t {               // keys of a block of 32 that exist
-      uint32_t m = it.c1 - t0 >= 32 ? 0xffffffffu : it.c1 <= t0 ? 0u : (1u << (it.c1 - t0)) - 1;
+    auto there = [&](int t) -> uint64_t {                  // keys of stage t that exist
+      const int t0 = it.c0 + t * SK, n = it.c1 - t0;
+      uint64_t m = n >= SK ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
       if (any_bad)
-        for (int half = 0; half < 2; ++half) {
-          const int t = min(t0 + 16 * half, it.c1 - 1);
-          if ((uint32_t)src.pages[t >> a.c.shift] >= (uint64_t)a.c.n_pages) m &= half ? 0x0000ffffu : 0xffff0000u;
+        for (int part = 0; part < 4; ++part) {
+          const int p = src.pages[min(t0 + 16 * part, it.c1 - 1) >> a.c.shift];
+          if ((uint32_t)p >= (uint64_t)a.c.n_pages) m &= ~(0xffffull << (16 * part));
         }
       return m;
     };
     Raw64<TYPE> raw;
     int pid[Raw64<TYPE>::N];
-    page_ids<TYPE>(pid, a, src, it.c0);
-    load_stage<TYPE>(raw, pid, a, src, it.c0);
-    page_ids<TYPE>(pid, a, src, it.c0 + SK);
-    write_stage<TYPE>(st[0], raw, tid);
-    load_stage<TYPE>(raw, pid, a, src, it.c0 + SK);
-    page_ids<TYPE>(pid, a, src, it.c0 + 2 * SK);
+    auto load = [&](int t) { load_stage<TYPE>(raw, pid, a, src, it.c0 + t * SK); };
+    auto ids = [&](int t) { page_ids<TYPE>(pid, a, src, it.c0 + t * SK); };
+    ids(0);
+    load(0);
+    ids(1);
+    write_stage<TYPE>(st[0], raw, wave, lane, there(0));
+    load(1);
+    ids(2);
+    write_stage<TYPE>(st[1], raw, wave, lane, there(1));
+    if (steps > 2) load(2);
+    if (steps > 3) ids(3);
     __syncthreads();
     // unit u: stage u / 2, block u % 2 (one key group), or stage u, block wk (two)
     const int units = WK == 1 ? 2 * steps : steps;
@@ -891,44 +931,60 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
       return st[(WK == 1 ? u >> 1 : u) & (NST - 1)].v + vlane + 32 * TV * (WK == 1 ? u & 1 : wk);
     };
     f32x16 s0 = {}, s1 = {};
-    bf16x8 p0[2], p1[2];
+    bf16x8 p0[2], p1[2], op[AHEAD + 1];
 #pragma unroll
     for (int x = 0; x < 2; ++x) p0[x] = p1[x] = zero8();
 #pragma unroll
-    for (int x = 0; x < 8; ++x) s0 = mfma32(slot_operand(2 * x, k_at(0), nullptr), r.q[x], s0);
-    write_stage<TYPE>(st[1], raw, tid);
-    if (steps > 2) load_stage<TYPE>(raw, pid, a, src, it.c0 + 2 * SK);
-    if (steps > 3) page_ids<TYPE>(pid, a, src, it.c0 + 3 * SK);
-    // The barrier before the last unit of stage t: stage t + 1 is whole, and
-    // every wave is through with the unit before, thus with stage t - 2 (and
-    // with one key group t - 1). The slot before unit 0 has no V yet: its P
-    // is zero, and unit 0's own block stands in for it.
-    auto stage_on = [&](int t) {
+    for (int x = 0; x < 8; ++x) s0 = mfma32(slot_operand(x, k_at(0), nullptr), r.q[x], s0);
+    // The slot before unit 0 has no V yet: its P is zero, and unit 0's own
+    // block stands in for it.
+    constexpr bool PRE = WK == 1;
+    if (PRE) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) op[i] = slot_operand(i, k_at(1), v_at(0));
+    }
+    auto stage_on = [&](int t) {                           // stage t + 2 into LDS, t + 3 on its way
       if (t + 2 >= steps) return;
-      write_stage<TYPE>(st[(t + 2) & (NST - 1)], raw, tid);
-      if (t + 3 < steps) load_stage<TYPE>(raw, pid, a, src, it.c0 + (t + 3) * SK);
-      if (t + 4 < steps) page_ids<TYPE>(pid, a, src, it.c0 + (t + 4) * SK);
+      write_stage<TYPE>(st[(t + 2) & (NST - 1)], raw, wave, lane, there(t + 2));
+      if (t + 3 < steps) load(t + 3);
+      if (t + 4 < steps) ids(t + 4);
     };
+    auto mask = [&](f32x16& s, int u) {
+      const uint64_t m = there(WK == 1 ? u >> 1 : u);
+      if (m != ~0ull) mask_unit(s, (uint32_t)(m >> (32 * (WK == 1 ? u & 1 : wk))), h);
+    };
+    // One key group, units 2 t and 2 t + 1 in step t: behind its barrier stage
+    // t + 1 is whole, and the one that takes stage t + 2 (t - 2's) has been
+    // read for the last time in step t - 1. Half the waves stage between their
+    // slots, half behind them: of the two waves on a SIMD one then computes
+    // while the other stages.
+    // Two key groups, unit u = stage u: behind the barrier of slot u stage
+    // u + 1 is whole, and everybody is through with slot u - 1, the last to
+    // read stage u - 2.
+    const bool late = WK == 1 && wave >= 4;
     for (int u = 0; u < units; u += 2) {
-      if (WK == 2) __syncthreads();
-      uint32_t seen = seen_of(it.c0 + (WK == 1 ? 32 * u : SK * u + 32 * wk));
+      if (WK == 2 || u > 0) __syncthreads();
       if (active) {
-        if (seen != 0xffffffffu) mask_unit(s0, seen, h);
-        slot<WL>(r, s0, s1, p1, p0, a.sc, k_at(u + 1), v_at(u > 0 ? u - 1 : 0));
+        mask(s0, u);
+        slot<WL, PRE>(r, op, s0, s1, p1, p0, a.sc, k_at(u + 1), v_at(u > 0 ? u - 1 : 0), k_at(u + 2), v_at(u));
       }
-      if (WK == 2) stage_on(u);
-      __syncthreads();
-      seen = seen_of(it.c0 + (WK == 1 ? 32 * (u + 1) : SK * (u + 1) + 32 * wk));
+      if (WK == 2) {
+        stage_on(u);
+        __syncthreads();
+      } else if (!late) {
+        stage_on(u >> 1);
+      }
       if (active) {
-        if (seen != 0xffffffffu) mask_unit(s1, seen, h);
-        slot<WL>(r, s1, s0, p0, p1, a.sc, k_at(u + 2), v_at(u));
+        mask(s1, u + 1);
+        slot<WL, PRE>(r, op, s1, s0, p0, p1, a.sc, k_at(u + 2), v_at(u), k_at(u + 3), v_at(u + 1));
       }
-      stage_on(WK == 1 ? u >> 1 : u + 1);
+      if (WK == 2) stage_on(u + 1);
+      else if (late) stage_on(u >> 1);
     }
     if (active) {
       const uint16_t* vp = v_at(units - 1);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) r.o[x & 3] = mfma32(slot_operand(2 * x + 1, nullptr, vp), p1[x >> 2], r.o[x & 3]);
+      for (int x = 0; x < 8; ++x) r.o[x & 3] = mfma32(slot_operand(8 + x, nullptr, vp), p1[x >> 2], r.o[x & 3]);
     }
     __syncthreads();
   }
