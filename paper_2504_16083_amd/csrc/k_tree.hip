@@ -649,13 +649,20 @@ struct __align__(16) Stage64 {
   uint16_t v[SK * TV];
 };
 
-template <int TYPE>
+template <int TYPE, int WK>
 struct Raw64 {                         // a thread's pieces of a stage: piece i is number tid + i * NTW
   static constexpr int CPR = Codec<TYPE>::ROW / 16;        // pieces a row
   static constexpr int N = SK * CPR / NTW > 0 ? SK * CPR / NTW : 1;
-  static constexpr int LIVE = SK * CPR < NTW ? SK * CPR / 64 : NTW / 64;   // waves with pieces
+  static constexpr int LIVE = SK * CPR < NTW ? SK * CPR / 64 : NTW / 64;   // waves that hold one of K and V
+  // E2M1 with two key groups: the first group's waves take K (in k), the
+  // second's V (in k too), as they wait for each other at every unit. With one
+  // group the waves that stage late are better off without (328 us for 340,
+  // 64 drafts over 262144 tokens, 32 heads on 8; 16 over 1M tokens, two
+  // groups: 435 us split, 466 not).
+  static constexpr bool SPLIT = LIVE < NTW / 64 && WK == 2;
   u32x4 k[N], v[N];
   uint32_t ks[N], vs[N];
+  typedef int Ids[N];                                      // page numbers
 };
 
 // Where a wave's pieces come from. Its 64 pieces i are 4, 8 or 16 whole rows,
@@ -667,57 +674,64 @@ struct KeySource {
   int zero;                            // in a vector register: keeps the page table's loads vector loads
 };
 
-template <int TYPE>
+template <int TYPE, int WK>
 __device__ __forceinline__ int first_key(int wave, int i) {
-  return (wave % Raw64<TYPE>::LIVE * 64 + i * NTW) / Raw64<TYPE>::CPR;
+  return (wave % Raw64<TYPE, WK>::LIVE * 64 + i * NTW) / Raw64<TYPE, WK>::CPR;
 }
 
 // The numbers stay in a vector register until they are used, a stage later: a
 // scalar load would share its counter with the LDS reads of the slots between.
-template <int TYPE>
-__device__ __forceinline__ void page_ids(int (&p)[Raw64<TYPE>::N], const TreeArgs& a, const KeySource& s, int t0) {
+template <int TYPE, int WK>
+__device__ __forceinline__ void page_ids(typename Raw64<TYPE, WK>::Ids& p, const TreeArgs& a, const KeySource& s, int t0) {
 #pragma unroll
-  for (int i = 0; i < Raw64<TYPE>::N; ++i)
-    p[i] = s.pages[(min(t0 + first_key<TYPE>(s.wave, i), s.c1 - 1) >> a.c.shift) + s.zero];
+  for (int i = 0; i < Raw64<TYPE, WK>::N; ++i)
+    p[i] = s.pages[(min(t0 + first_key<TYPE, WK>(s.wave, i), s.c1 - 1) >> a.c.shift) + s.zero];
 }
 
 // Pages outside the cache are read as page 0, which is there; their keys are
 // masked, and their V staged as zero.
-template <int TYPE>
-__device__ __forceinline__ void load_stage(Raw64<TYPE>& r, const int (&p)[Raw64<TYPE>::N], const TreeArgs& a,
+template <int TYPE, int WK>
+__device__ __forceinline__ void load_stage(Raw64<TYPE, WK>& r, const typename Raw64<TYPE, WK>::Ids& p, const TreeArgs& a,
                                            const KeySource& s, int t0) {
-  typedef Raw64<TYPE> R;
-  if (R::LIVE < NTW / 64 && s.wave >= R::LIVE) return;
+  typedef Raw64<TYPE, WK> R;
+  if (!R::SPLIT && R::LIVE < NTW / 64 && s.wave >= R::LIVE) return;
+  const bool second = s.wave >= R::LIVE;                   // of SPLIT
+  static_assert(!R::SPLIT || R::LIVE == NTW / 128, "half the waves take K, half V");
 #pragma unroll
   for (int i = 0; i < R::N; ++i) {
-    const int t = t0 + first_key<TYPE>(s.wave, i);
+    const int t = t0 + first_key<TYPE, WK>(s.wave, i);
     const int id = __builtin_amdgcn_readfirstlane(p[i]);
     const int64_t page = (uint32_t)id < (uint64_t)a.c.n_pages ? id : 0;
     const int in = (s.head << a.c.shift) + (t & ((1 << a.c.shift) - 1));
     const int64_t at = page * a.c.page_stride + (int64_t)in * Codec<TYPE>::ROW;
-    r.k[i] = reinterpret_cast<const u32x4*>(a.c.k + at)[s.lane];
-    r.v[i] = reinterpret_cast<const u32x4*>(a.c.v + at)[s.lane];
+    r.k[i] = reinterpret_cast<const u32x4*>((second ? a.c.v : a.c.k) + at)[s.lane];
+    if constexpr (!R::SPLIT) r.v[i] = reinterpret_cast<const u32x4*>(a.c.v + at)[s.lane];
     if constexpr (Codec<TYPE>::SCALED) {
       const int64_t sat = page * a.c.scale_stride + (int64_t)in * 4;
-      r.ks[i] = reinterpret_cast<const uint32_t*>((const uint8_t*)a.c.ks + sat)[s.lane / R::CPR];
-      r.vs[i] = reinterpret_cast<const uint32_t*>((const uint8_t*)a.c.vs + sat)[s.lane / R::CPR];
+      r.ks[i] = reinterpret_cast<const uint32_t*>((const uint8_t*)(second ? a.c.vs : a.c.ks) + sat)[s.lane / R::CPR];
+      if constexpr (!R::SPLIT) r.vs[i] = reinterpret_cast<const uint32_t*>((const uint8_t*)a.c.vs + sat)[s.lane / R::CPR];
     }
   }
 }
 
 // `there`: the stage's keys that exist; the others weigh nothing, whatever
 // their places hold.
-template <int TYPE>
-__device__ __forceinline__ void write_stage(Stage64& st, const Raw64<TYPE>& r, int wave, int lane, uint64_t there) {
-  typedef Raw64<TYPE> R;
-  if (R::LIVE < NTW / 64 && wave >= R::LIVE) return;
+template <int TYPE, int WK>
+__device__ __forceinline__ void write_stage(Stage64& st, const Raw64<TYPE, WK>& r, int wave, int lane, uint64_t there) {
+  typedef Raw64<TYPE, WK> R;
+  if (!R::SPLIT && R::LIVE < NTW / 64 && wave >= R::LIVE) return;
 #pragma unroll
   for (int i = 0; i < R::N; ++i) {
-    const int key = first_key<TYPE>(wave, i) + lane / R::CPR, piece = lane % R::CPR;
-    put_piece<TYPE>(&st.k[key * TK], r.k[i], r.ks[i], piece);
-    u32x4 v = r.v[i];
-    if (there != ~0ull && !(there >> key & 1)) v = u32x4{};
-    put_piece<TYPE>(&st.v[key * TV], v, there != ~0ull && !(there >> key & 1) ? 0u : r.vs[i], piece);
+    const int key = first_key<TYPE, WK>(wave, i) + lane / R::CPR, piece = lane % R::CPR;
+    const bool ok = there == ~0ull || (there >> key & 1);
+    const u32x4 none = {};
+    if constexpr (R::SPLIT) {
+      if (wave < R::LIVE) put_piece<TYPE>(&st.k[key * TK], r.k[i], r.ks[i], piece);
+      else put_piece<TYPE>(&st.v[key * TV], ok ? r.k[i] : none, ok ? r.ks[i] : 0u, piece);
+    } else {
+      put_piece<TYPE>(&st.k[key * TK], r.k[i], r.ks[i], piece);
+      put_piece<TYPE>(&st.v[key * TV], ok ? r.v[i] : none, ok ? r.vs[i] : 0u, piece);
+    }
   }
 }
 
@@ -809,6 +823,7 @@ __device__ __forceinline__ void slot(Rows& r, bf16x8 (&op)[AHEAD + 1], f32x16& s
                                      const uint16_t* vp, const uint16_t* kn, const uint16_t* vn) {
   SoftState z;
   const f32x16 zero = {};
+  __builtin_amdgcn_s_setprio(1);       // before the SIMD's other wave while that stages
   if (!PRE) {
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) op[i] = slot_operand(i, kp, vp);
@@ -830,6 +845,7 @@ __device__ __forceinline__ void slot(Rows& r, bf16x8 (&op)[AHEAD + 1], f32x16& s
     for (; pc < end; ++pc) soft_piece<WL>(pc, s_sm, sc, r, p_sm, z);
     __builtin_amdgcn_sched_barrier(0);
   }
+  __builtin_amdgcn_s_setprio(0);
   if (__any(z.alpha != 1.0f)) rescale(r, z.alpha);         // O holds PV up to unit u - 1, by the old maximum
 }
 
@@ -887,8 +903,8 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
   r.m = -INFINITY;
   r.l = r.lo = 0.0f;
 
-  // stages, an even number of units a wave: what lies behind c1 is staged as nothing
-  const int steps = (it.c1 - it.c0 + SK * WK - 1) / (SK * WK) * WK;
+  // stages, an even number: what lies behind c1 is staged as nothing
+  const int steps = (it.c1 - it.c0 + 2 * SK - 1) / (2 * SK) * 2;
   if (steps > 0) {
     int zero = 0;
     asm("" : "+v"(zero));
@@ -908,19 +924,22 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
         }
       return m;
     };
-    Raw64<TYPE> raw;
-    int pid[Raw64<TYPE>::N];
-    auto load = [&](int t) { load_stage<TYPE>(raw, pid, a, src, it.c0 + t * SK); };
-    auto ids = [&](int t) { page_ids<TYPE>(pid, a, src, it.c0 + t * SK); };
+    // Two stages are on their way in registers, in turn: a load has two steps to arrive.
+    Raw64<TYPE, WK> even, odd;
+    typename Raw64<TYPE, WK>::Ids pid;
+    auto load = [&](Raw64<TYPE, WK>& raw, int t) { load_stage<TYPE, WK>(raw, pid, a, src, it.c0 + t * SK); };
+    auto ids = [&](int t) { page_ids<TYPE, WK>(pid, a, src, it.c0 + t * SK); };
     ids(0);
-    load(0);
+    load(even, 0);
     ids(1);
-    write_stage<TYPE>(st[0], raw, wave, lane, there(0));
-    load(1);
+    load(odd, 1);
     ids(2);
-    write_stage<TYPE>(st[1], raw, wave, lane, there(1));
-    if (steps > 2) load(2);
-    if (steps > 3) ids(3);
+    write_stage<TYPE, WK>(st[0], even, wave, lane, there(0));
+    load(even, 2);
+    ids(3);
+    write_stage<TYPE, WK>(st[1], odd, wave, lane, there(1));
+    load(odd, 3);
+    ids(4);
     __syncthreads();
     // unit u: stage u / 2, block u % 2 (one key group), or stage u, block wk (two)
     const int units = WK == 1 ? 2 * steps : steps;
@@ -943,17 +962,18 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) op[i] = slot_operand(i, k_at(1), v_at(0));
     }
-    auto stage_on = [&](int t) {                           // stage t + 2 into LDS, t + 3 on its way
+    auto stage_on = [&](Raw64<TYPE, WK>& raw, int t) {         // stage t + 2 into LDS, t + 4 on its way
       if (t + 2 >= steps) return;
-      write_stage<TYPE>(st[(t + 2) & (NST - 1)], raw, wave, lane, there(t + 2));
-      if (t + 3 < steps) load(t + 3);
-      if (t + 4 < steps) ids(t + 4);
+      write_stage<TYPE, WK>(st[(t + 2) & (NST - 1)], raw, wave, lane, there(t + 2));
+      if (t + 4 >= steps) return;
+      load(raw, t + 4);
+      ids(t + 5);
     };
     auto mask = [&](f32x16& s, int u) {
       const uint64_t m = there(WK == 1 ? u >> 1 : u);
       if (m != ~0ull) mask_unit(s, (uint32_t)(m >> (32 * (WK == 1 ? u & 1 : wk))), h);
     };
-    // One key group, units 2 t and 2 t + 1 in step t: behind its barrier stage
+    // One key group, units 2 t and 2 t + 1 in step t: behind the barrier before it stage
     // t + 1 is whole, and the one that takes stage t + 2 (t - 2's) has been
     // read for the last time in step t - 1. Half the waves stage between their
     // slots, half behind them: of the two waves on a SIMD one then computes
@@ -962,24 +982,37 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
     // u + 1 is whole, and everybody is through with slot u - 1, the last to
     // read stage u - 2.
     const bool late = WK == 1 && wave >= 4;
-    for (int u = 0; u < units; u += 2) {
-      if (WK == 2 || u > 0) __syncthreads();
-      if (active) {
-        mask(s0, u);
-        slot<WL, PRE>(r, op, s0, s1, p1, p0, a.sc, k_at(u + 1), v_at(u > 0 ? u - 1 : 0), k_at(u + 2), v_at(u));
-      }
-      if (WK == 2) {
-        stage_on(u);
+    auto first_slot = [&](int u) {                         // u even: scores in s0
+      if (!active) return;
+      mask(s0, u);
+      slot<WL, PRE>(r, op, s0, s1, p1, p0, a.sc, k_at(u + 1), v_at(max(u - 1, 0)), k_at(u + 2), v_at(u));
+    };
+    auto second_slot = [&](int u) {
+      if (!active) return;
+      mask(s1, u);
+      slot<WL, PRE>(r, op, s1, s0, p0, p1, a.sc, k_at(u + 1), v_at(u - 1), k_at(u + 2), v_at(u));
+    };
+    if (WK == 2) {
+      for (int u = 0; u < units; u += 2) {
         __syncthreads();
-      } else if (!late) {
-        stage_on(u >> 1);
+        first_slot(u);
+        stage_on(even, u);
+        __syncthreads();
+        second_slot(u + 1);
+        stage_on(odd, u + 1);
       }
-      if (active) {
-        mask(s1, u + 1);
-        slot<WL, PRE>(r, op, s1, s0, p0, p1, a.sc, k_at(u + 2), v_at(u), k_at(u + 3), v_at(u + 1));
+    } else {
+      auto step = [&](Raw64<TYPE, WK>& raw, int t) {
+        first_slot(2 * t);
+        if (!late) stage_on(raw, t);
+        second_slot(2 * t + 1);
+        if (late) stage_on(raw, t);
+        __syncthreads();
+      };
+      for (int t = 0; t < steps; t += 2) {
+        step(even, t);
+        step(odd, t + 1);
       }
-      if (WK == 2) stage_on(u + 1);
-      else if (late) stage_on(u >> 1);
     }
     if (active) {
       const uint16_t* vp = v_at(units - 1);
