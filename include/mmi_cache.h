@@ -61,6 +61,11 @@ typedef struct mmi_rope_cfg {
                                     and scaling (factor still sets m of PARTS), or NULL */
 } mmi_rope_cfg;
 
+/* The frequencies f_i of a configuration: HOST array [rot_dim / 2]. Computing
+ * them takes longer than a short call's other host work; a program that calls
+ * mmi_rope for single tokens keeps them in inv_freq. */
+int mmi_rope_freq(const mmi_rope_cfg* cfg, double* inv_freq);
+
 /* Rotates Q [S, Hq, 128] and K [S, Hkv, 128] of `prob` (its strides; v, o and
  * modality are not read) into q_out and k_out, laid out as q and k. q_out = q
  * or k_out = k rotates in place; otherwise an output overlaps no input. q or

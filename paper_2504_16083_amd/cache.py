@@ -50,7 +50,7 @@ class mmi_tree(ct.Structure):
                 ("scale", ct.c_float), ("reserved", ct.c_int32)]
 
 
-SYMBOLS = ["mmi_rope", "mmi_cache_write", "mmi_cache_read", "mmi_tree_workspace", "mmi_tree_attention"]
+SYMBOLS = ["mmi_rope_freq", "mmi_rope", "mmi_cache_write", "mmi_cache_read", "mmi_tree_workspace", "mmi_tree_attention"]
 
 _lib = None
 
@@ -61,6 +61,7 @@ def lib():
         L = mmi.lib()
         vp, i64, sz, P = ct.c_void_p, ct.c_int64, ct.c_size_t, ct.POINTER
         sig = {
+            "mmi_rope_freq": [P(mmi_rope_cfg), P(ct.c_double)],
             "mmi_rope": [vp, P(mmi.mmi_problem), P(mmi_rope_cfg), vp, vp, vp, vp, vp, vp],
             "mmi_cache_write": [vp, P(mmi_cache), vp, i64, i64, vp, i64, i64, vp, i64, vp],
             "mmi_cache_read": [vp, P(mmi_cache), vp, i64, vp, i64, i64, vp, i64, i64, vp],
@@ -132,15 +133,21 @@ class RopeCfg:
         if len(sections) != 3:
             raise ValueError("sections are three numbers of pairs")
         self.axes = 3 if any(sections) else 1
-        table = None
+        table = (ct.c_double * 64)()
         if inv_freq is not None:
-            if len(inv_freq) != rot_dim // 2:
+            if len(inv_freq) != rot_dim // 2 or len(inv_freq) > 64:
                 raise ValueError(f"{len(inv_freq)} frequencies for {rot_dim // 2} pairs")
-            table = (ct.c_double * max(1, len(inv_freq)))(*[float(f) for f in inv_freq])
+            table[:len(inv_freq)] = [float(f) for f in inv_freq]
         self._table = table
         self.c = [mmi_rope_cfg(rot_dim, LAYOUTS[layout], SCALINGS[scaling], inverse, (ct.c_int32 * 3)(*sections), 0,
-                               theta, factor, orig_len, beta_fast, beta_slow, attn_factor, table)
+                               theta, factor, orig_len, beta_fast, beta_slow, attn_factor,
+                               None if inv_freq is None else table)
                   for inverse in (0, 1)]
+        if inv_freq is None:                       # once, not with every call
+            _check(lib().mmi_rope_freq(ct.byref(self.c[0]), table))
+            for c in self.c:
+                c.inv_freq = ct.cast(table, ct.POINTER(ct.c_double))
+        self.ref = [ct.byref(c) for c in self.c]
 
 
 def mmi_rope(ctx, cfg, q=None, k=None, pos=None, q_out=None, k_out=None, inverse=False, stream=None):
@@ -149,33 +156,30 @@ def mmi_rope(ctx, cfg, q=None, k=None, pos=None, q_out=None, k_out=None, inverse
     [3, S] with sections; None: 0 .. S-1. inverse: the gradient's rotation."""
     if q is None and k is None:
         raise ValueError("neither q nor k")
-    p = mmi.mmi_problem()
-    p.S = (q if q is not None else k).shape[0]
-    p.D, p.block, p.Hq, p.Hkv = D, 64, 1, 1
+    S = (k if q is None else q).shape[0]
+    Hq = Hkv = 1
+    qs = ks = (0, 0)
+    qp = kp = qo = ko = None
     if k is not None:
-        p.k_stride_s, p.k_stride_h = strides = _rows(ctx, "k", k, p.S, None)
-        p.Hkv = k.shape[1]
-        if k_out is None:
-            k_out = k
-        elif _rows(ctx, "k_out", k_out, p.S, p.Hkv) != strides:
-            raise ValueError("k_out must have the strides of k")
-        p.Hq = p.Hkv
+        ks, Hkv = _rows(ctx, "k", k, S, None), k.shape[1]
+        Hq = Hkv
+        kp = ko = k.data_ptr()
+        if k_out is not None:
+            if _rows(ctx, "k_out", k_out, S, Hkv) != ks:
+                raise ValueError("k_out must have the strides of k")
+            ko = k_out.data_ptr()
     if q is not None:
-        p.q_stride_s, p.q_stride_h = strides = _rows(ctx, "q", q, p.S, None)
-        p.Hq = q.shape[1]
-        if k is None:
-            p.Hkv = 1
-        if q_out is None:
-            q_out = q
-        elif _rows(ctx, "q_out", q_out, p.S, p.Hq) != strides:
-            raise ValueError("q_out must have the strides of q")
+        qs, Hq = _rows(ctx, "q", q, S, None), q.shape[1]
+        qp = qo = q.data_ptr()
+        if q_out is not None:
+            if _rows(ctx, "q_out", q_out, S, Hq) != qs:
+                raise ValueError("q_out must have the strides of q")
+            qo = q_out.data_ptr()
     pp = None
     if pos is not None:
-        pp = _array(ctx, "pos", pos, torch.int32, (p.S,) if cfg.axes == 1 else (3, p.S))
-    _check(lib().mmi_rope(ctx.h, ct.byref(p), ct.byref(cfg.c[1 if inverse else 0]), pp,
-                          None if q is None else q.data_ptr(), None if k is None else k.data_ptr(),
-                          None if q is None else q_out.data_ptr(), None if k is None else k_out.data_ptr(),
-                          _stream(ctx, stream)))
+        pp = _array(ctx, "pos", pos, torch.int32, (S,) if cfg.axes == 1 else (3, S))
+    p = mmi.mmi_problem(S, Hq, Hkv, D, 64, *qs, *ks)
+    _check(lib().mmi_rope(ctx.h, ct.byref(p), cfg.ref[1 if inverse else 0], pp, qp, kp, qo, ko, _stream(ctx, stream)))
 
 
 # ------------------------------------------------------------------ the cache

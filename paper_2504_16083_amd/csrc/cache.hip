@@ -35,29 +35,19 @@ void strides(int64_t& ss, int64_t& sh, int H, const char* name) {
   if (ss > ((int64_t)1 << 40) || sh > ((int64_t)1 << 40)) fail(MMI_ERR_UNSUPPORTED, "%s strides exceed 2^40", name);
 }
 
+constexpr double TWO_PI = 6.283185307179586476925286766559;
 constexpr int ROW_BYTES[4] = {256, 128, 128, 64};
 
 }  // namespace
 
-RopeArgs rope_args(const mmi_problem& p, const mmi_rope_cfg* cfg, const int32_t* pos, const void* q, const void* k,
-                   void* q_out, void* k_out) {
+// Radians a position of every pair, and the factor of cos and sin.
+double rope_freq(const mmi_rope_cfg* cfg, double* freq) {
   if (!cfg) fail(MMI_ERR_INVALID_ARG, "rope config is NULL");
   const mmi_rope_cfg& c = *cfg;
   if (c.rot_dim < 16 || c.rot_dim > D || c.rot_dim % 16)
     fail(MMI_ERR_UNSUPPORTED, "rot_dim %d is not a multiple of 16 in [16, 128]", c.rot_dim);
-  if (c.layout != MMI_ROPE_HALF && c.layout != MMI_ROPE_INTERLEAVED)
-    fail(MMI_ERR_BAD_CONFIG, "unknown rope layout %d", c.layout);
   if (c.scaling < MMI_ROPE_SCALE_NONE || c.scaling > MMI_ROPE_SCALE_PARTS)
     fail(MMI_ERR_BAD_CONFIG, "unknown rope scaling %d", c.scaling);
-  if (c.inverse != 0 && c.inverse != 1) fail(MMI_ERR_BAD_CONFIG, "inverse must be 0 or 1");
-  if (c.reserved) fail(MMI_ERR_INVALID_ARG, "reserved must be 0");
-  const int half = c.rot_dim / 2;
-  int64_t sum = 0;
-  for (int s : c.sections) {
-    if (s < 0) fail(MMI_ERR_BAD_CONFIG, "a section is negative");
-    sum += s;
-  }
-  if (sum != 0 && sum != half) fail(MMI_ERR_BAD_CONFIG, "sections add up to %lld of %d pairs", (long long)sum, half);
   if (!c.inv_freq && !(c.theta > 0 && std::isfinite(c.theta))) fail(MMI_ERR_BAD_CONFIG, "theta must be positive");
   if (c.scaling != MMI_ROPE_SCALE_NONE && !(c.factor >= 1 && std::isfinite(c.factor)))
     fail(MMI_ERR_BAD_CONFIG, "factor must be at least 1");
@@ -67,6 +57,43 @@ RopeArgs rope_args(const mmi_problem& p, const mmi_rope_cfg* cfg, const int32_t*
     fail(MMI_ERR_BAD_CONFIG, "orig_len must be positive and beta_fast > beta_slow >= 0");
   if (!(c.attn_factor >= 0 && std::isfinite((float)c.attn_factor)))
     fail(MMI_ERR_BAD_CONFIG, "attn_factor must not be negative");
+  double theta = c.theta;
+  if (c.scaling == MMI_ROPE_SCALE_NTK) theta *= std::pow(c.factor, (double)c.rot_dim / (c.rot_dim - 2));
+  for (int i = 0; i < c.rot_dim / 2; ++i) {
+    double f;
+    if (c.inv_freq) {
+      f = c.inv_freq[i];
+    } else {
+      f = std::pow(theta, -2.0 * i / c.rot_dim);
+      if (c.scaling == MMI_ROPE_SCALE_LINEAR) f /= c.factor;
+      if (c.scaling == MMI_ROPE_SCALE_PARTS) {
+        const double g = std::fmin(std::fmax((c.orig_len * f / TWO_PI - c.beta_slow) / (c.beta_fast - c.beta_slow),
+                                             0.0), 1.0);
+        f *= g + (1.0 - g) / c.factor;
+      }
+    }
+    if (!(f >= 0 && std::isfinite(f))) fail(MMI_ERR_BAD_CONFIG, "frequency %d is not a finite positive number", i);
+    freq[i] = f;
+  }
+  return c.attn_factor > 0 ? c.attn_factor : c.scaling == MMI_ROPE_SCALE_PARTS ? 0.1 * std::log(c.factor) + 1.0 : 1.0;
+}
+
+RopeArgs rope_args(const mmi_problem& p, const mmi_rope_cfg* cfg, const int32_t* pos, const void* q, const void* k,
+                   void* q_out, void* k_out) {
+  double freq[D / 2];
+  const double m = rope_freq(cfg, freq);
+  const mmi_rope_cfg& c = *cfg;
+  if (c.layout != MMI_ROPE_HALF && c.layout != MMI_ROPE_INTERLEAVED)
+    fail(MMI_ERR_BAD_CONFIG, "unknown rope layout %d", c.layout);
+  if (c.inverse != 0 && c.inverse != 1) fail(MMI_ERR_BAD_CONFIG, "inverse must be 0 or 1");
+  if (c.reserved) fail(MMI_ERR_INVALID_ARG, "reserved must be 0");
+  const int half = c.rot_dim / 2;
+  int64_t sum = 0;
+  for (int s : c.sections) {
+    if (s < 0) fail(MMI_ERR_BAD_CONFIG, "a section is negative");
+    sum += s;
+  }
+  if (sum != 0 && sum != half) fail(MMI_ERR_BAD_CONFIG, "sections add up to %lld of %d pairs", (long long)sum, half);
   if (!q && !k) fail(MMI_ERR_INVALID_ARG, "q and k are NULL");
   if (!q != !q_out || !k != !k_out) fail(MMI_ERR_INVALID_ARG, "an input without its output, or the other way round");
   if (q) { aligned(q, 16, "q"); aligned(q_out, 16, "q_out"); }
@@ -85,29 +112,10 @@ RopeArgs rope_args(const mmi_problem& p, const mmi_rope_cfg* cfg, const int32_t*
   a.inverse = c.inverse;
   a.sec1 = sum ? c.sections[0] : half;
   a.sec2 = sum ? c.sections[0] + c.sections[1] : half;
-  const double m = c.attn_factor > 0 ? c.attn_factor
-                   : c.scaling == MMI_ROPE_SCALE_PARTS ? 0.1 * std::log(c.factor) + 1.0 : 1.0;
   a.m = (float)m;
-  const double two_pi = 6.283185307179586476925286766559;
-  double theta = c.theta;
-  if (!c.inv_freq && c.scaling == MMI_ROPE_SCALE_NTK)
-    theta *= std::pow(c.factor, (double)c.rot_dim / (c.rot_dim - 2));
   for (int i = 0; i < half; ++i) {
-    double f;
-    if (c.inv_freq) {
-      f = c.inv_freq[i];
-    } else {
-      f = std::pow(theta, -2.0 * i / c.rot_dim);
-      if (c.scaling == MMI_ROPE_SCALE_LINEAR) f /= c.factor;
-      if (c.scaling == MMI_ROPE_SCALE_PARTS) {
-        const double g = std::fmin(std::fmax((c.orig_len * f / two_pi - c.beta_slow) / (c.beta_fast - c.beta_slow),
-                                             0.0), 1.0);
-        f *= g + (1.0 - g) / c.factor;
-      }
-    }
-    if (!(f >= 0 && std::isfinite(f))) fail(MMI_ERR_BAD_CONFIG, "frequency %d is not a finite positive number", i);
-    const double t = f / two_pi;
-    a.turn[i] = (uint64_t)std::ldexp(t - std::floor(t), 64);   // below 2^64: the fraction is at most 1 - 2^-53
+    const double t = freq[i] * (1.0 / TWO_PI), part = t - std::floor(t);
+    a.turn[i] = (uint64_t)(part * 18446744073709551616.0);   // below 2^64: the fraction is at most 1 - 2^-53
   }
   return a;
 }

@@ -69,6 +69,7 @@ hipError_t launch_tree(const TreeArgs& a, int type, int rows, hipStream_t st);
 
 // ---------------------------------------------------------------- cache.hip
 // Host checks (they throw Error) and the records for the launches.
+double rope_freq(const mmi_rope_cfg* cfg, double* freq);
 RopeArgs rope_args(const mmi_problem& p, const mmi_rope_cfg* cfg, const int32_t* pos, const void* q, const void* k,
                    void* q_out, void* k_out);
 CacheDev cache_dev(const mmi_cache* c);

@@ -74,18 +74,8 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* before, int64_
 struct Item {
   int b, first, chunks, chunk, tile, head;   // sequence, its first item, its chunks; this one's chunk, tile, head
   int c0, c1;                                // cached tokens
+  Seq seq;
 };
-
-// Items of the batch with chunks of this length.
-template <int ROWS, int NT>
-__device__ __forceinline__ int64_t count_items(const TreeArgs& a, int chunk, int64_t* sh64) {
-  int64_t n = 0, before;
-  for (int b = threadIdx.x; b < a.n_seq; b += NT) {
-    const Seq s = sequence(a, b);
-    n += (int64_t)((s.T * a.g + ROWS - 1) / ROWS) * max(1, (s.L + chunk - 1) / chunk);
-  }
-  return block_scan<NT>(n, &before, sh64) * a.c.Hkv;
-}
 
 // Item `it` of the batch. The chunk length follows from the work of the whole
 // batch (cached tokens x tiles x heads, cut into `target` parts), so long
@@ -94,64 +84,128 @@ __device__ __forceinline__ int64_t count_items(const TreeArgs& a, int chunk, int
 // parts; as `target` of them run at once, the chunks are then made longer
 // until all start together (a second round of a few items takes as long as
 // the first: a ragged batch of 32 decoded tokens took 74 us for 65).
+__device__ __forceinline__ int chunk_of(int64_t work, int64_t parts) {
+  const int64_t len = work < (1 << 30) ? ((int)work + (int)parts - 1) / (int)parts : (work + parts - 1) / parts;
+  return (int)((max(len, (int64_t)1) + CHUNK - 1) / CHUNK * CHUNK);
+}
+
+template <int ROWS>
+__device__ __forceinline__ int tiles_of(const TreeArgs& a, const Seq& s) { return (s.T * a.g + ROWS - 1) / ROWS; }
+
+// Chunk of a batch with this work (cached tokens x tiles) and these tiles;
+// count(chunk): its tiles x chunks.
+template <typename F>
+__device__ __forceinline__ int choose_chunk(const TreeArgs& a, int64_t work, int64_t tiles, F&& count) {
+  work *= a.c.Hkv;
+  const int chunk = chunk_of(work, a.target);
+  const int64_t items = count(chunk) * a.c.Hkv, units = tiles * a.c.Hkv;
+  if (items <= a.target || units >= a.target) return chunk;
+  // at most units + work / chunk items: the second length always fits
+  const int longer = chunk_of(work, max((int64_t)1, a.target * (int64_t)a.target / items));
+  const int safe = chunk_of(work, a.target - units);
+  return longer < safe && count(longer) * a.c.Hkv <= a.target ? longer : safe;
+}
+
+__device__ __forceinline__ void set_item(const TreeArgs& a, Item& r, int it, int b, int first, int tiles, int chunk,
+                                         const Seq& s) {
+  const int at = it - first;
+  r.b = b;
+  r.first = first;
+  r.seq = s;
+  r.chunks = max(1, (s.L + chunk - 1) / chunk);
+  r.chunk = at / (tiles * a.c.Hkv);
+  const int rest = at - r.chunk * tiles * a.c.Hkv;
+  r.head = rest / tiles;
+  r.tile = rest - r.head * tiles;
+  r.c0 = min(s.L, r.chunk * chunk);
+  r.c1 = (int)min((int64_t)s.L, (int64_t)r.c0 + chunk);
+}
+
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
+  return x;
+}
+
+// Up to 64 sequences every wave finds the item by itself, a sequence a lane;
+// more are scanned by the workgroup, NT at a time.
 template <int ROWS, int NT>
 __device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, int64_t* sh64, int* sh) {
   const int tid = threadIdx.x;
-  int64_t work = 0, units = 0, before;
-  for (int b = tid; b < a.n_seq; b += NT) {
-    const Seq s = sequence(a, b);
-    const int tiles = (s.T * a.g + ROWS - 1) / ROWS;
-    work += (int64_t)tiles * s.L;
-    units += tiles;
-  }
-  work = block_scan<NT>(work, &before, sh64) * a.c.Hkv;
-  auto chunk_of = [&](int64_t parts) -> int {
-    const int64_t len = (work + parts - 1) / parts;
-    return (int)((max(len, (int64_t)1) + CHUNK - 1) / CHUNK * CHUNK);
-  };
-  int chunk = chunk_of(a.target);
-  int64_t items = count_items<ROWS, NT>(a, chunk, sh64);
-  if (items > a.target) {
-    units = block_scan<NT>(units, &before, sh64) * a.c.Hkv;
-    if (units < a.target) {        // at most units + work / chunk items: the second length always fits
-      const int longer = chunk_of(max((int64_t)1, a.target * a.target / items)), safe = chunk_of(a.target - units);
-      chunk = longer < safe && count_items<ROWS, NT>(a, longer, sh64) <= a.target ? longer : safe;
-    }
-  }
-  if (tid == 0) sh[0] = -1;
-  int64_t base = 0;
-  for (int b0 = 0; b0 < a.n_seq; b0 += NT) {
-    const int b = b0 + tid;
+  if (a.n_seq == 1) {
+    const Seq s = sequence(a, 0);
+    const int tiles = tiles_of<ROWS>(a, s);
+    auto count = [&](int chunk) -> int64_t { return (int64_t)tiles * max(1, (s.L + chunk - 1) / chunk); };
+    const int chunk = choose_chunk(a, (int64_t)tiles * s.L, tiles, count);
+    if (it >= count(chunk) * a.c.Hkv) return false;
+    set_item(a, r, it, 0, 0, tiles, chunk, s);
+  } else if (a.n_seq <= 64) {
+    const int lane = tid & 63;
     Seq s = {0, 0, 0};
-    if (b < a.n_seq) s = sequence(a, b);
-    const int tiles = (s.T * a.g + ROWS - 1) / ROWS, chunks = max(1, (s.L + chunk - 1) / chunk);
-    const int64_t n = (int64_t)tiles * a.c.Hkv * chunks;
-    const int64_t all = block_scan<NT>(n, &before, sh64);
-    const int64_t at = it - base - before;
-    if (n > 0 && at >= 0 && at < n) {
-      const int tile = (int)(at % tiles), head = (int)(at / tiles % a.c.Hkv);
-      const int c = (int)(at / ((int64_t)tiles * a.c.Hkv));
-      sh[0] = b; sh[1] = (int)(base + before); sh[2] = chunks; sh[3] = c; sh[4] = tile; sh[5] = head;
-      sh[6] = min(s.L, c * chunk);
-      sh[7] = (int)min((int64_t)s.L, (int64_t)(c + 1) * chunk);
-      if (at == 0) {
-        a.rec[2 * b] = it;
-        a.rec[2 * b + 1] = chunks;
-      }
+    if (lane < a.n_seq) s = sequence(a, lane);
+    const int tiles = tiles_of<ROWS>(a, s);
+    int64_t work = (int64_t)tiles * s.L;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
+    // fewer than 2^31 items: each has a workgroup
+    auto count = [&](int chunk) -> int64_t { return wave_sum(tiles * max(1, (s.L + chunk - 1) / chunk)); };
+    const int chunk = choose_chunk(a, work, wave_sum(tiles), count);
+    const int n = tiles * a.c.Hkv * max(1, (s.L + chunk - 1) / chunk);
+    int end = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(end, d);
+      if (lane >= d) end += y;
     }
-    base += all;
-    if (base > it) break;
+    const uint64_t mine = __ballot(it >= end - n && it < end);
+    if (!mine) return false;
+    const int b = __builtin_ctzll(mine);
+    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, b); };
+    const Seq sb = {of(s.row0), of(s.T), of(s.L)};
+    set_item(a, r, it, b, of(end - n), of(tiles), chunk, sb);
+  } else {
+    int64_t work = 0, tiles = 0, before;
+    for (int b = tid; b < a.n_seq; b += NT) {
+      const Seq s = sequence(a, b);
+      work += (int64_t)tiles_of<ROWS>(a, s) * s.L;
+      tiles += tiles_of<ROWS>(a, s);
+    }
+    work = block_scan<NT>(work, &before, sh64);
+    tiles = block_scan<NT>(tiles, &before, sh64);
+    auto count = [&](int chunk) -> int64_t {
+      int64_t n = 0, bef;
+      for (int b = tid; b < a.n_seq; b += NT) {
+        const Seq s = sequence(a, b);
+        n += (int64_t)tiles_of<ROWS>(a, s) * max(1, (s.L + chunk - 1) / chunk);
+      }
+      return block_scan<NT>(n, &bef, sh64);
+    };
+    const int chunk = choose_chunk(a, work, tiles, count);
+    if (tid == 0) sh[0] = -1;
+    int64_t base = 0;
+    for (int b0 = 0; b0 < a.n_seq && base <= it; b0 += NT) {
+      const int b = b0 + tid;
+      Seq s = {0, 0, 0};
+      if (b < a.n_seq) s = sequence(a, b);
+      const int64_t n = (int64_t)tiles_of<ROWS>(a, s) * a.c.Hkv * max(1, (s.L + chunk - 1) / chunk);
+      const int64_t all = block_scan<NT>(n, &before, sh64);
+      if (it >= base + before && it < base + before + n) {
+        sh[0] = b;
+        sh[1] = (int)(base + before);
+      }
+      base += all;
+    }
+    __syncthreads();
+    const int b = __builtin_amdgcn_readfirstlane(sh[0]);
+    if (b < 0) return false;
+    const Seq s = sequence(a, b);
+    set_item(a, r, it, b, __builtin_amdgcn_readfirstlane(sh[1]), tiles_of<ROWS>(a, s), chunk, s);
   }
-  __syncthreads();
-  r.b = __builtin_amdgcn_readfirstlane(sh[0]);
-  r.first = __builtin_amdgcn_readfirstlane(sh[1]);
-  r.chunks = __builtin_amdgcn_readfirstlane(sh[2]);
-  r.chunk = __builtin_amdgcn_readfirstlane(sh[3]);
-  r.tile = __builtin_amdgcn_readfirstlane(sh[4]);
-  r.head = __builtin_amdgcn_readfirstlane(sh[5]);
-  r.c0 = __builtin_amdgcn_readfirstlane(sh[6]);
-  r.c1 = __builtin_amdgcn_readfirstlane(sh[7]);
-  return r.b >= 0;
+  if (it == r.first && tid == 0) {         // for the join
+    a.rec[2 * r.b] = it;
+    a.rec[2 * r.b + 1] = r.chunks;
+  }
+  return true;
 }
 
 // One 16-byte piece as bfloat16 into a staged row.
@@ -470,7 +524,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
   __shared__ int sh[8];
   Item it;
   if (!find_item<ROWS, 256>(a, blockIdx.x, it, sh64, sh)) return;
-  const Seq sq = sequence(a, it.b);
+  const Seq sq = it.seq;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int c = lane & 15, q = lane >> 4;
   uint16_t* const v = vs + wave * KB * TV;
@@ -874,7 +928,7 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
   __shared__ int sh[8];
   Item it;
   if (!find_item<ROWS, NTW>(a, blockIdx.x, it, sh64, sh)) return;
-  const Seq sq = sequence(a, it.b);
+  const Seq sq = it.seq;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int wr = wave % WR, wk = wave / WR;
   const int c = lane & 31, h = lane >> 5;
@@ -1122,50 +1176,69 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
 
 // Joins the partials of the sequences that were cut into chunks. Workgroup
 // (row of a sequence's rows, KV head and sequence): 8 groups of 32 lanes take
-// every eighth partial, 4 channels a lane, and meet in LDS.
+// every eighth partial, 4 channels a lane, JU of them in flight, and meet in
+// LDS.
+constexpr int JU = 4;
+
 template <int ROWS>
 __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   const int rows = a.max_rows * a.g, row = blockIdx.x % rows;
   const int head = blockIdx.x / rows % a.c.Hkv, b = blockIdx.x / rows / a.c.Hkv;
   const Seq sq = sequence(a, b);
+  const int first = a.rec[2 * b], chunks = a.rec[2 * b + 1];   // what they were if the sequence has no rows
   const int tok = row / a.g;
-  if (tok >= sq.T) return;
-  const int first = a.rec[2 * b], chunks = a.rec[2 * b + 1];
-  if (chunks <= 1) return;
+  if (tok >= sq.T || chunks <= 1) return;
   const int tiles = (sq.T * a.g + ROWS - 1) / ROWS;
   const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
-  auto slot = [&](int p) {
-    return ((int64_t)first + ((int64_t)p * a.c.Hkv + head) * tiles + row / ROWS) * ROWS + row % ROWS;
-  };
-  __shared__ float4 so[8][32];
-  __shared__ float sm[8][3];
-  float m = -INFINITY;
-  for (int p = grp; p < chunks; p += 8) m = fmaxf(m, a.part_ml[slot(p) * 4]);
-  if (lane == 0) sm[grp][0] = m;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < 8; ++w) m = fmaxf(m, sm[w][0]);
+  const int64_t at0 = ((int64_t)first + (int64_t)head * tiles + row / ROWS) * ROWS + row % ROWS;
+  const int64_t step = (int64_t)a.c.Hkv * tiles * ROWS;        // from chunk to chunk
+  __shared__ float4 so[8][32], sml[8];
+  float m = -INFINITY, l = 0.0f, lo = 0.0f;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  float l = 0.0f, lo = 0.0f;
-  for (int p = grp; p < chunks; p += 8) {
-    const float4 e = *reinterpret_cast<const float4*>(a.part_ml + slot(p) * 4);
-    const float4 y = *reinterpret_cast<const float4*>(a.part_o + slot(p) * D + 4 * lane);
-    const float f = e.x == -INFINITY ? 0.0f : fast_exp2(e.x - m);
-    lo += e.y * f;
-    l += e.z * f;
-    o.x += y.x * f; o.y += y.y * f; o.z += y.z * f; o.w += y.w * f;
+  for (int p0 = grp; p0 < chunks; p0 += 8 * JU) {
+    float4 e[JU], y[JU];
+#pragma unroll
+    for (int u = 0; u < JU; ++u) {
+      const int64_t at = at0 + min(p0 + 8 * u, chunks - 1) * step;
+      e[u] = *reinterpret_cast<const float4*>(a.part_ml + at * 4);
+      y[u] = *reinterpret_cast<const float4*>(a.part_o + at * D + 4 * lane);
+    }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < JU; ++u)
+      if (p0 + 8 * u < chunks) mn = fmaxf(mn, e[u].x);
+    const float f = m == -INFINITY ? 0.0f : fast_exp2(m - mn);
+    l *= f; lo *= f;
+    o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+    m = mn;
+#pragma unroll
+    for (int u = 0; u < JU; ++u) {
+      if (p0 + 8 * u >= chunks) break;
+      const float w = e[u].x == -INFINITY ? 0.0f : fast_exp2(e[u].x - m);
+      lo += e[u].y * w;
+      l += e[u].z * w;
+      o.x += y[u].x * w; o.y += y[u].y * w; o.z += y[u].z * w; o.w += y[u].w * w;
+    }
   }
   so[grp][lane] = o;
-  __syncthreads();
-  if (lane == 0) { sm[grp][1] = lo; sm[grp][2] = l; }
+  if (lane == 0) sml[grp] = make_float4(m, lo, l, 0.0f);
   __syncthreads();
   if (grp) return;
+  float4 part[8];
 #pragma unroll
-  for (int w = 1; w < 8; ++w) {
+  for (int w = 0; w < 8; ++w) {
+    part[w] = sml[w];
+    m = fmaxf(m, part[w].x);
+  }
+  l = lo = 0.0f;
+  o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    const float f = part[w].x == -INFINITY ? 0.0f : fast_exp2(part[w].x - m);
     const float4 y = so[w][lane];
-    o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
-    lo += sm[w][1];
-    l += sm[w][2];
+    lo += part[w].y * f;
+    l += part[w].z * f;
+    o.x += y.x * f; o.y += y.y * f; o.z += y.z * f; o.w += y.w * f;
   }
   const float inv = lo > 0.0f ? 1.0f / lo : lo == 0.0f ? 0.0f : lo;
   const int qh = head * a.g + row - tok * a.g;

@@ -1617,6 +1617,15 @@ struct OnDevice {
   }
 };
 
+int mmi_rope_freq(const mmi_rope_cfg* cfg, double* inv_freq) {
+  return guarded([&] {
+    double freq[D / 2];
+    rope_freq(cfg, freq);
+    if (!inv_freq) fail(MMI_ERR_INVALID_ARG, "inv_freq is NULL");
+    std::memcpy(inv_freq, freq, sizeof(double) * (size_t)(cfg->rot_dim / 2));
+  });
+}
+
 int mmi_rope(mmi_ctx* ctx, const mmi_problem* prob, const mmi_rope_cfg* cfg, const int32_t* pos, const void* q,
              const void* k, void* q_out, void* k_out, void* stream) {
   return guarded([&] {
