@@ -242,6 +242,7 @@ struct Rows {                          // a wave's 32 rows
   f32x16 o[4];
   bf16x8 q[8];
   float m, l, lo;                      // maximum (log2 units) of a row; sums of this lane's P (fp32, bf16)
+  float base, most;                    // m, or 0 while it is -inf; what a unit's sum may be before m has to move
 };
 
 __device__ __forceinline__ float half_max(float x) {
@@ -813,58 +814,60 @@ __device__ __forceinline__ void mask_unit(f32x16& s, uint32_t seen, int h) {
 template <typename T>
 __device__ __forceinline__ void pin(T& x) { asm volatile("" : "+v"(x)); }
 
-// The softmax of a unit in pieces that fit between MFMAs: 0, 1 maxima of 8
-// scores, 2 the running maximum, 3-18 one exponential each, 19, 20 packing
-// and the sum of the packed, 21 the sums.
-constexpr int PIECES = 22;
+// The softmax of a unit in pieces that fit between MFMAs: one exponential
+// each, and after eight their packing and the sum of the packed. It takes the
+// running maximum as it is and looks at no score: the sums tell, at the slot's
+// end, where some row's scores have passed its maximum by so much (P of up to
+// 2^12 do no harm) that it has to move, and soft_again makes P anew. (Finding
+// a unit's maxima first put 20 dependent instructions before the exponentials
+// of every slot: NEWFIG.)
+constexpr int PIECES = 18;
+constexpr float MOST = 4096.0f;
 struct SoftState {
-  float mx, base, alpha, rs, ro;
+  float e[8], rs, ro;
 };
 
 template <bool WL>
-__device__ __forceinline__ void soft_piece(int piece, f32x16& s, float sc, Rows& r, bf16x8 (&p)[2], SoftState& z) {
-  if (piece < 2) {
-    float mx = s[8 * piece];
-#pragma unroll
-    for (int x = 1; x < 8; ++x) mx = fmaxf(mx, s[8 * piece + x]);
-    z.mx = piece == 0 ? mx : fmaxf(z.mx, mx);
-    pin(z.mx);
-  } else if (piece == 2) {
-    const float mx = half_max(z.mx) * sc;                  // sc > 0
-    const bool move = __any(mx > r.m + SLACK);
-    const float mn = move ? fmaxf(r.m, mx) : r.m;
-    z.alpha = r.m == mn ? 1.0f : fast_exp2(r.m - mn);
-    r.m = mn;
-    z.base = mn == -INFINITY ? 0.0f : mn;                  // nothing seen yet: every P is 2^-inf = 0
-    z.rs = z.ro = 0.0f;
-    pin(z.base);
-  } else if (piece < 19) {
-    const int x = piece - 3;
-    float e = fast_exp2(fmaf(s[x], sc, -z.base));
+__device__ __forceinline__ void soft_piece(int piece, const f32x16& s, float sc, const Rows& r, bf16x8 (&p)[2],
+                                           SoftState& z) {
+  const int half = piece / 9, x = piece % 9;
+  if (piece == 0) z.rs = z.ro = 0.0f;
+  if (x < 8) {
+    float e = fast_exp2(fmaf(s[8 * half + x], sc, -r.base));
     pin(e);
-    s[x] = e;
+    z.e[x] = e;
     if (WL) z.rs += e;
-  } else if (piece < 21) {
-    const int half = piece - 19;
+  } else {
     const bf16e2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
-    for (int x = 0; x < 8; ++x) p[half][x] = (__bf16)s[8 * half + x];   // rounded for the product: O is divided by the sum of these
+    for (int i = 0; i < 8; ++i) p[half][i] = (__bf16)z.e[i];   // rounded for the product; O is divided by the sum of these
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-      z.ro = __builtin_amdgcn_fdot2_f32_bf16(bf16e2{p[half][2 * x], p[half][2 * x + 1]}, one, z.ro, false);
+    for (int i = 0; i < 4; ++i)
+      z.ro = __builtin_amdgcn_fdot2_f32_bf16(bf16e2{p[half][2 * i], p[half][2 * i + 1]}, one, z.ro, false);
     pin(z.ro);
     pin(p[half]);
-  } else {
-    if (WL) r.l = r.l * z.alpha + z.rs;
-    r.lo = r.lo * z.alpha + z.ro;
   }
 }
 
-__device__ __forceinline__ void rescale(Rows& r, float alpha) {
+// The unit's maxima move m, with O, l and lo; P and its sums once more.
+template <bool WL>
+__device__ __forceinline__ void soft_again(const f32x16& s, float sc, Rows& r, bf16x8 (&p)[2], SoftState& z) {
+  float mx = s[0];
+#pragma unroll
+  for (int x = 1; x < 16; ++x) mx = fmaxf(mx, s[x]);
+  mx = half_max(mx) * sc;                                  // sc > 0
+  const float m = fmaxf(r.m, mx), alpha = r.m == m ? 1.0f : fast_exp2(r.m - m);
+  r.m = m;
+  r.base = m == -INFINITY ? 0.0f : m;                      // nothing seen yet: every P is 2^-inf = 0
+  r.most = m == -INFINITY ? -1.0f : MOST;
+  r.l *= alpha;
+  r.lo *= alpha;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int x = 0; x < 16; ++x) r.o[dt][x] *= alpha;
+#pragma unroll
+  for (int pc = 0; pc < PIECES; ++pc) soft_piece<WL>(pc, s, sc, r, p, z);
 }
 
 constexpr int AHEAD = 3;
@@ -900,7 +903,10 @@ __device__ __forceinline__ void slot(Rows& r, bf16x8 (&op)[AHEAD + 1], f32x16& s
     __builtin_amdgcn_sched_barrier(0);
   }
   __builtin_amdgcn_s_setprio(0);
-  if (__any(z.alpha != 1.0f)) rescale(r, z.alpha);         // O holds PV up to unit u - 1, by the old maximum
+  // O holds PV up to unit u - 1, by the maximum of unit u - 1
+  if (__any(z.ro > r.most)) soft_again<WL>(s_sm, sc, r, p_sm, z);
+  if (WL) r.l += z.rs;
+  r.lo += z.ro;
 }
 
 // A staged block of 32 keys, nothing overlapped.
@@ -912,9 +918,9 @@ __device__ __forceinline__ void unit_alone(Rows& r, uint32_t seen, float sc, int
   mask_unit(s, seen, h);
   SoftState z;
   bf16x8 p[2];
-#pragma unroll
-  for (int pc = 0; pc < PIECES; ++pc) soft_piece<true>(pc, s, sc, r, p, z);
-  rescale(r, z.alpha);
+  soft_again<true>(s, sc, r, p, z);
+  r.l += z.rs;
+  r.lo += z.ro;
 #pragma unroll
   for (int x = 0; x < 8; ++x) r.o[x & 3] = mfma32(slot_operand(8 + x, kp, vp), p[x >> 2], r.o[x & 3]);
 }
@@ -955,7 +961,8 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
     for (int x = 0; x < 16; ++x) r.o[dt][x] = 0.0f;
   r.m = -INFINITY;
-  r.l = r.lo = 0.0f;
+  r.l = r.lo = r.base = 0.0f;
+  r.most = -1.0f;
 
   // stages, an even number: what lies behind c1 is staged as nothing
   const int steps = (it.c1 - it.c0 + 2 * SK - 1) / (2 * SK) * 2;
