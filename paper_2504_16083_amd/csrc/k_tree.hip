@@ -201,6 +201,9 @@ __device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, in
     const Seq s = sequence(a, b);
     set_item(a, r, it, b, __builtin_amdgcn_readfirstlane(sh[1]), tiles_of<ROWS>(a, s), chunk, s);
   }
+  // the same in every lane: into scalar registers, or every branch on them is a divergent one
+  for (int* x : {&r.b, &r.first, &r.chunks, &r.chunk, &r.tile, &r.head, &r.c0, &r.c1, &r.seq.row0, &r.seq.T, &r.seq.L})
+    *x = __builtin_amdgcn_readfirstlane(*x);
   if (it == r.first && tid == 0) {         // for the join
     a.rec[2 * r.b] = it;
     a.rec[2 * r.b + 1] = r.chunks;
@@ -351,15 +354,23 @@ struct Raw32 {                                        // a block of 32 keys as i
   uint32_t seen;                                      // keys that exist
 };
 
+// Numbers of the two pages (16 keys each) of the block from token t on, read a
+// block before its loads: they wait for nothing then. `zero` in a vector
+// register keeps these vector loads, whose counter the LDS reads do not share.
+__device__ __forceinline__ void block_pages(int (&p)[2], const TreeArgs& a, const int32_t* pages, int t, int len,
+                                            int zero) {
+#pragma unroll
+  for (int half = 0; half < 2; ++half) p[half] = pages[(min(t + 16 * half, len - 1) >> a.c.shift) + zero];
+}
+
 template <int TYPE>
-__device__ __forceinline__ void load_block(Raw32<TYPE>& r, const TreeArgs& a, const int32_t* pages, int head, int t0,
+__device__ __forceinline__ void load_block(Raw32<TYPE>& r, const TreeArgs& a, const int (&pages)[2], int head, int t0,
                                            int len, int lane) {
   typedef Raw32<TYPE> R;
   r.seen = len - t0 >= KB ? 0xffffffffu : (1u << (len - t0)) - 1;
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {              // 16 keys lie in one page
-    const int t = t0 + 16 * half;
-    const int p = t < len ? pages[t >> a.c.shift] : -1;
+  for (int half = 0; half < 2; ++half) {
+    const int t = t0 + 16 * half, p = __builtin_amdgcn_readfirstlane(pages[half]);
     const bool ok = (uint32_t)p < (uint64_t)a.c.n_pages;
     if (!ok) r.seen &= half ? 0x0000ffffu : 0xffff0000u;
     const int64_t page = ok ? p : 0;
@@ -556,8 +567,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
 
   const int32_t* pages = a.pages + (int64_t)it.b * a.max_pages;
   Raw32<TYPE> raw;
+  int pid[2], zero = 0;
+  asm("" : "+v"(zero));
   int t0 = it.c0 + KB * wave;
-  if (t0 < it.c1) load_block<TYPE>(raw, a, pages, it.head, t0, it.c1, lane);
+  if (t0 < it.c1) {
+    block_pages(pid, a, pages, t0, it.c1, zero);
+    load_block<TYPE>(raw, a, pid, it.head, t0, it.c1, lane);
+    block_pages(pid, a, pages, t0 + 4 * KB, it.c1, zero);
+  }
   for (; t0 < it.c1; t0 += 4 * KB) {
     uint32_t seen[RN];
 #pragma unroll
@@ -575,7 +592,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
         for (int x = 0; x < 4; ++x) s[n][half] = mfma16(op[x], r.q[n][x], s[n][half]);
       }
     }
-    if (t0 + 4 * KB < it.c1) load_block<TYPE>(raw, a, pages, it.head, t0 + 4 * KB, it.c1, lane);
+    if (t0 + 4 * KB < it.c1) {
+      load_block<TYPE>(raw, a, pid, it.head, t0 + 4 * KB, it.c1, lane);
+      block_pages(pid, a, pages, t0 + 8 * KB, it.c1, zero);
+    }
     wave_fence();
     attend_few<RN>(r, s, v, seen, a.sc, q, vlane);
     wave_fence();
