@@ -13,11 +13,14 @@
 // more the products (k_tree_wide). A sequence of several chunks leaves
 // partials that k_tree_join merges in a fixed order.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.hpp"
 #include "codec.hpp"
 
 namespace mmi {
+
+#define INLINE __attribute__((always_inline))   // of lambdas: called twice they would become functions of memory
 
 constexpr int KB = 32;                 // keys of a block
 constexpr int TK = 136, TV = 160;      // bf16 a staged K / V row: operand reads without bank conflicts
@@ -724,21 +727,27 @@ struct __align__(16) Stage64 {
   uint16_t v[SK * TV];
 };
 
-template <int TYPE, int WK>
+template <int TYPE>
 struct Raw64 {                         // a thread's pieces of a stage: piece i is number tid + i * NTW
   static constexpr int CPR = Codec<TYPE>::ROW / 16;        // pieces a row
   static constexpr int N = SK * CPR / NTW > 0 ? SK * CPR / NTW : 1;
   static constexpr int LIVE = SK * CPR < NTW ? SK * CPR / 64 : NTW / 64;   // waves that hold one of K and V
-  // E2M1 with two key groups: the first group's waves take K (in k), the
-  // second's V (in k too), as they wait for each other at every unit. With one
-  // group the waves that stage late are better off without (328 us for 340,
-  // 64 drafts over 262144 tokens, 32 heads on 8; 16 over 1M tokens, two
-  // groups: 435 us split, 466 not).
-  static constexpr bool SPLIT = LIVE < NTW / 64 && WK == 2;
+  // E2M1: the first waves take K (in k), the others V (in k too). Leaving all
+  // to the first ones took 330 us where this takes 314 (64 drafts over 262144
+  // tokens, 32 heads on 8).
+  static constexpr bool SPLIT = LIVE < NTW / 64;
   u32x4 k[N], v[N];
   uint32_t ks[N], vs[N];
   typedef int Ids[N];                                      // page numbers
 };
+
+// A pointer that is the same in every lane, kept in scalar registers: a load
+// from it then takes a lane's offset in one register, not an address in two.
+template <typename T>
+__device__ __forceinline__ const __attribute__((address_space(1))) T* scalar(const void* p) {
+  asm("" : "+s"(p));
+  return (const __attribute__((address_space(1))) T*)p;
+}
 
 // Where a wave's pieces come from. Its 64 pieces i are 4, 8 or 16 whole rows,
 // which lie in one page and follow each other: one page number and scalar base
@@ -746,58 +755,57 @@ struct Raw64 {                         // a thread's pieces of a stage: piece i 
 struct KeySource {
   const int32_t* pages;
   int head, c0, c1, wave, lane;
-  int zero;                            // in a vector register: keeps the page table's loads vector loads
+  uint32_t zero;                       // in a vector register: keeps the page table's loads vector loads
 };
 
-template <int TYPE, int WK>
+template <int TYPE>
 __device__ __forceinline__ int first_key(int wave, int i) {
-  return (wave % Raw64<TYPE, WK>::LIVE * 64 + i * NTW) / Raw64<TYPE, WK>::CPR;
+  return (wave % Raw64<TYPE>::LIVE * 64 + i * NTW) / Raw64<TYPE>::CPR;
 }
 
 // The numbers stay in a vector register until they are used, a stage later: a
 // scalar load would share its counter with the LDS reads of the slots between.
-template <int TYPE, int WK>
-__device__ __forceinline__ void page_ids(typename Raw64<TYPE, WK>::Ids& p, const TreeArgs& a, const KeySource& s, int t0) {
+template <int TYPE>
+__device__ __forceinline__ void page_ids(typename Raw64<TYPE>::Ids& p, const TreeArgs& a, const KeySource& s, int t0) {
 #pragma unroll
-  for (int i = 0; i < Raw64<TYPE, WK>::N; ++i)
-    p[i] = s.pages[(min(t0 + first_key<TYPE, WK>(s.wave, i), s.c1 - 1) >> a.c.shift) + s.zero];
+  for (int i = 0; i < Raw64<TYPE>::N; ++i)
+    p[i] = scalar<int32_t>(s.pages + (min(t0 + first_key<TYPE>(s.wave, i), s.c1 - 1) >> a.c.shift))[s.zero];
 }
 
 // Pages outside the cache are read as page 0, which is there; their keys are
 // masked, and their V staged as zero.
-template <int TYPE, int WK>
-__device__ __forceinline__ void load_stage(Raw64<TYPE, WK>& r, const typename Raw64<TYPE, WK>::Ids& p, const TreeArgs& a,
+template <int TYPE>
+__device__ __forceinline__ void load_stage(Raw64<TYPE>& r, const typename Raw64<TYPE>::Ids& p, const TreeArgs& a,
                                            const KeySource& s, int t0) {
-  typedef Raw64<TYPE, WK> R;
-  if (!R::SPLIT && R::LIVE < NTW / 64 && s.wave >= R::LIVE) return;
+  typedef Raw64<TYPE> R;
   const bool second = s.wave >= R::LIVE;                   // of SPLIT
   static_assert(!R::SPLIT || R::LIVE == NTW / 128, "half the waves take K, half V");
 #pragma unroll
   for (int i = 0; i < R::N; ++i) {
-    const int t = t0 + first_key<TYPE, WK>(s.wave, i);
+    const int t = t0 + first_key<TYPE>(s.wave, i);
     const int id = __builtin_amdgcn_readfirstlane(p[i]);
     const int64_t page = (uint32_t)id < (uint64_t)a.c.n_pages ? id : 0;
     const int in = (s.head << a.c.shift) + (t & ((1 << a.c.shift) - 1));
     const int64_t at = page * a.c.page_stride + (int64_t)in * Codec<TYPE>::ROW;
-    r.k[i] = reinterpret_cast<const u32x4*>((second ? a.c.v : a.c.k) + at)[s.lane];
-    if constexpr (!R::SPLIT) r.v[i] = reinterpret_cast<const u32x4*>(a.c.v + at)[s.lane];
+    r.k[i] = scalar<u32x4>((second ? a.c.v : a.c.k) + at)[(uint32_t)s.lane];
+    if constexpr (!R::SPLIT) r.v[i] = scalar<u32x4>(a.c.v + at)[(uint32_t)s.lane];
     if constexpr (Codec<TYPE>::SCALED) {
       const int64_t sat = page * a.c.scale_stride + (int64_t)in * 4;
-      r.ks[i] = reinterpret_cast<const uint32_t*>((const uint8_t*)(second ? a.c.vs : a.c.ks) + sat)[s.lane / R::CPR];
-      if constexpr (!R::SPLIT) r.vs[i] = reinterpret_cast<const uint32_t*>((const uint8_t*)a.c.vs + sat)[s.lane / R::CPR];
+      const uint32_t row = (uint32_t)s.lane / R::CPR;
+      r.ks[i] = scalar<uint32_t>((const uint8_t*)(second ? a.c.vs : a.c.ks) + sat)[row];
+      if constexpr (!R::SPLIT) r.vs[i] = scalar<uint32_t>((const uint8_t*)a.c.vs + sat)[row];
     }
   }
 }
 
 // `there`: the stage's keys that exist; the others weigh nothing, whatever
 // their places hold.
-template <int TYPE, int WK>
-__device__ __forceinline__ void write_stage(Stage64& st, const Raw64<TYPE, WK>& r, int wave, int lane, uint64_t there) {
-  typedef Raw64<TYPE, WK> R;
-  if (!R::SPLIT && R::LIVE < NTW / 64 && wave >= R::LIVE) return;
+template <int TYPE>
+__device__ __forceinline__ void write_stage(Stage64& st, const Raw64<TYPE>& r, int wave, int lane, uint64_t there) {
+  typedef Raw64<TYPE> R;
 #pragma unroll
   for (int i = 0; i < R::N; ++i) {
-    const int key = first_key<TYPE, WK>(wave, i) + lane / R::CPR, piece = lane % R::CPR;
+    const int key = first_key<TYPE>(wave, i) + lane / R::CPR, piece = lane % R::CPR;
     const bool ok = there == ~0ull || (there >> key & 1);
     const u32x4 none = {};
     if constexpr (R::SPLIT) {
@@ -840,7 +848,8 @@ __device__ __forceinline__ void pin(T& x) { asm volatile("" : "+v"(x)); }
 // end, where some row's scores have passed its maximum by so much (P of up to
 // 2^12 do no harm) that it has to move, and soft_again makes P anew. (Finding
 // a unit's maxima first put 20 dependent instructions before the exponentials
-// of every slot: NEWFIG.)
+// of every slot: six ragged trees 402 us for 383, 16 drafts over 1M tokens in
+// four bits 451 for 425.)
 constexpr int PIECES = 18;
 constexpr float MOST = 4096.0f;
 struct SoftState {
@@ -987,7 +996,7 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
   // stages, an even number: what lies behind c1 is staged as nothing
   const int steps = (it.c1 - it.c0 + 2 * SK - 1) / (2 * SK) * 2;
   if (steps > 0) {
-    int zero = 0;
+    uint32_t zero = 0;
     asm("" : "+v"(zero));
     const KeySource src = {a.pages + (int64_t)it.b * a.max_pages, it.head, it.c0, it.c1, wave, lane, zero};
     // pages outside the cache are rare enough to ask once for the whole chunk
@@ -995,7 +1004,7 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
     for (int p = (it.c0 >> a.c.shift) + tid; p <= (it.c1 - 1) >> a.c.shift; p += NTW)
       bad |= (uint32_t)src.pages[p] >= (uint64_t)a.c.n_pages;
     const bool any_bad = __syncthreads_or(bad);
-    auto there = [&](int t) -> uint64_t {                  // keys of stage t that exist
+    auto there = [&](int t) INLINE -> uint64_t {                  // keys of stage t that exist
       const int t0 = it.c0 + t * SK, n = it.c1 - t0;
       uint64_t m = n >= SK ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
       if (any_bad)
@@ -1006,28 +1015,33 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
       return m;
     };
     // Two stages are on their way in registers, in turn: a load has two steps to arrive.
-    Raw64<TYPE, WK> even, odd;
-    typename Raw64<TYPE, WK>::Ids pid;
-    auto load = [&](Raw64<TYPE, WK>& raw, int t) { load_stage<TYPE, WK>(raw, pid, a, src, it.c0 + t * SK); };
-    auto ids = [&](int t) { page_ids<TYPE, WK>(pid, a, src, it.c0 + t * SK); };
+    Raw64<TYPE> even, odd;
+    typename Raw64<TYPE>::Ids pid;
+    auto load = [&](Raw64<TYPE>& raw, int t) INLINE { load_stage<TYPE>(raw, pid, a, src, it.c0 + t * SK); };
+    auto ids = [&](int t) INLINE { page_ids<TYPE>(pid, a, src, it.c0 + t * SK); };
     ids(0);
     load(even, 0);
     ids(1);
     load(odd, 1);
-    ids(2);
-    write_stage<TYPE, WK>(st[0], even, wave, lane, there(0));
-    load(even, 2);
-    ids(3);
-    write_stage<TYPE, WK>(st[1], odd, wave, lane, there(1));
-    load(odd, 3);
-    ids(4);
+    ids(min(2, steps - 1));
+    write_stage<TYPE>(st[0], even, wave, lane, there(0));
+    load(even, min(2, steps - 1));
+    ids(min(3, steps - 1));
+    write_stage<TYPE>(st[1], odd, wave, lane, there(1));
+    // the numbers of the next stage before the loads of this one, here as below
+    typename Raw64<TYPE>::Ids next;
+    page_ids<TYPE>(next, a, src, it.c0 + min(4, steps - 1) * SK);
+    __builtin_amdgcn_sched_barrier(0);
+    load(odd, min(3, steps - 1));
+#pragma unroll
+    for (int i = 0; i < Raw64<TYPE>::N; ++i) pid[i] = next[i];
     __syncthreads();
     // unit u: stage u / 2, block u % 2 (one key group), or stage u, block wk (two)
     const int units = WK == 1 ? 2 * steps : steps;
-    auto k_at = [&](int u) -> const uint16_t* {
+    auto k_at = [&](int u) INLINE -> const uint16_t* {
       return st[(WK == 1 ? u >> 1 : u) & (NST - 1)].k + klane + 32 * TK * (WK == 1 ? u & 1 : wk);
     };
-    auto v_at = [&](int u) -> const uint16_t* {
+    auto v_at = [&](int u) INLINE -> const uint16_t* {
       return st[(WK == 1 ? u >> 1 : u) & (NST - 1)].v + vlane + 32 * TV * (WK == 1 ? u & 1 : wk);
     };
     f32x16 s0 = {}, s1 = {};
@@ -1043,32 +1057,34 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) op[i] = slot_operand(i, k_at(1), v_at(0));
     }
-    auto stage_on = [&](Raw64<TYPE, WK>& raw, int t) {         // stage t + 2 into LDS, t + 4 on its way
-      if (t + 2 >= steps) return;
-      write_stage<TYPE, WK>(st[(t + 2) & (NST - 1)], raw, wave, lane, there(t + 2));
-      if (t + 4 >= steps) return;
-      load(raw, t + 4);
-      ids(t + 5);
+    // Stage t + 2 into LDS, t + 4 on its way. Nothing here is left out at the
+    // end (the last stage is loaded again, from the caches): where loads are
+    // issued on some paths only, the compiler waits for all of them. The next
+    // page numbers are asked for before the loads, and wait for none of them.
+    auto stage_on = [&](Raw64<TYPE>& raw, int t) INLINE {
+      write_stage<TYPE>(st[(t + 2) & (NST - 1)], raw, wave, lane, there(t + 2));
+      page_ids<TYPE>(next, a, src, it.c0 + min(t + 5, steps - 1) * SK);
+      __builtin_amdgcn_sched_barrier(0);
+      load(raw, min(t + 4, steps - 1));
+#pragma unroll
+      for (int i = 0; i < Raw64<TYPE>::N; ++i) pid[i] = next[i];
     };
-    auto mask = [&](f32x16& s, int u) {
+    auto mask = [&](f32x16& s, int u) INLINE {
       const uint64_t m = there(WK == 1 ? u >> 1 : u);
       if (m != ~0ull) mask_unit(s, (uint32_t)(m >> (32 * (WK == 1 ? u & 1 : wk))), h);
     };
-    // One key group, units 2 t and 2 t + 1 in step t: behind the barrier before it stage
-    // t + 1 is whole, and the one that takes stage t + 2 (t - 2's) has been
-    // read for the last time in step t - 1. Half the waves stage between their
-    // slots, half behind them: of the two waves on a SIMD one then computes
-    // while the other stages.
+    // One key group, units 2 t and 2 t + 1 in step t: behind the barrier before
+    // it stage t + 1 is whole, and the one that takes stage t + 2 (t - 2's) has
+    // been read for the last time in step t - 1.
     // Two key groups, unit u = stage u: behind the barrier of slot u stage
     // u + 1 is whole, and everybody is through with slot u - 1, the last to
     // read stage u - 2.
-    const bool late = WK == 1 && wave >= 4;
-    auto first_slot = [&](int u) {                         // u even: scores in s0
+    auto first_slot = [&](int u) INLINE {                         // u even: scores in s0
       if (!active) return;
       mask(s0, u);
       slot<WL, PRE>(r, op, s0, s1, p1, p0, a.sc, k_at(u + 1), v_at(max(u - 1, 0)), k_at(u + 2), v_at(u));
     };
-    auto second_slot = [&](int u) {
+    auto second_slot = [&](int u) INLINE {
       if (!active) return;
       mask(s1, u);
       slot<WL, PRE>(r, op, s1, s0, p0, p1, a.sc, k_at(u + 1), v_at(u - 1), k_at(u + 2), v_at(u));
@@ -1083,11 +1099,10 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
         stage_on(odd, u + 1);
       }
     } else {
-      auto step = [&](Raw64<TYPE, WK>& raw, int t) {
+      auto step = [&](Raw64<TYPE>& raw, int t) INLINE {
         first_slot(2 * t);
-        if (!late) stage_on(raw, t);
+        stage_on(raw, t);
         second_slot(2 * t + 1);
-        if (late) stage_on(raw, t);
         __syncthreads();
       };
       for (int t = 0; t < steps; t += 2) {
