@@ -69,12 +69,12 @@ __device__ __forceinline__ bf16x8 decode8(uint32_t w0, uint32_t w1, float s) {
     r[0] = a[0]; r[1] = a[1]; r[2] = b[0]; r[3] = b[1];
     r[4] = c[0]; r[5] = c[1]; r[6] = d[0]; r[7] = d[1];
   } else {
-    // bytes + 128 convert to fp32 in one instruction each; (b + 128) s - 128 s is exact
+    // bytes + 128 convert to fp32 in one instruction each (b s + (128 s) would
+    // save one more, but 128 s is no number for the largest scales)
     const uint32_t u0 = w0 ^ 0x80808080u, u1 = w1 ^ 0x80808080u;
-    const float off = -128.0f * s;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      r[e] = (__bf16)fmaf((float)((e < 4 ? u0 : u1) >> (8 * (e & 3)) & 255u), s, off);
+      r[e] = (__bf16)(((float)((e < 4 ? u0 : u1) >> (8 * (e & 3)) & 255u) - 128.0f) * s);
   }
   return r;
 }
