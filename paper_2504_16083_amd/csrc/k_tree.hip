@@ -1227,10 +1227,12 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
   const int rows = a.max_rows * a.g, row = blockIdx.x % rows;
   const int head = blockIdx.x / rows % a.c.Hkv, b = blockIdx.x / rows / a.c.Hkv;
   const Seq sq = sequence(a, b);
-  const int first = a.rec[2 * b], chunks = a.rec[2 * b + 1];   // what they were if the sequence has no rows
+  const int first = a.rec[2 * b], chunks = a.rec[2 * b + 1];
   const int tok = row / a.g;
-  if (tok >= sq.T || chunks <= 1) return;
-  const int tiles = (sq.T * a.g + ROWS - 1) / ROWS;
+  const int tiles = tiles_of<ROWS>(a, sq);
+  // A sequence without rows, or (row_start not ascending) behind the items that
+  // were launched, has no record: whatever the workspace held is no index.
+  if (tok >= sq.T || chunks <= 1 || first < 0 || first + (int64_t)chunks * a.c.Hkv * tiles > a.items) return;
   const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
   const int64_t at0 = ((int64_t)first + (int64_t)head * tiles + row / ROWS) * ROWS + row % ROWS;
   const int64_t step = (int64_t)a.c.Hkv * tiles * ROWS;        // from chunk to chunk

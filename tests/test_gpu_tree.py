@@ -150,6 +150,22 @@ def test_bad_pages_lengths_and_rows(ctx):
     assert (o[9:13] != 7).any()
 
 
+def test_row_start_that_does_not_ascend(ctx):
+    """Sequences that claim the same rows again and again: more tiles than n_rows announces. Nothing outside the
+    tensors and the workspace is read or written, whatever the workspace held."""
+    from paper_2504_16083_amd import cache as KV
+    b = Batch("fp8", [900] * 12, [256] + [0] * 11, 7, 1, 16, seed=14, behind=3)
+    b.tree.row_start.copy_(torch.tensor([0] + [256, 0] * 6, dtype=torch.int32))
+    ws = b.workspace(ctx)
+    for fill in (0x7f, 0xff, 0x01):
+        big = torch.full((ws.numel() + 8192,), fill, dtype=torch.uint8, device="cuda")
+        o, lse = b.outputs()
+        KV.mmi_tree_attention(ctx, b.cache, b.tree, b.q, b.k, b.v, o, big[4096:-4096], lse=lse)
+        torch.cuda.synchronize()
+        assert (big[:4096] == fill).all() and (big[-4096:] == fill).all()
+        assert (o[256:] == 7).all() and (lse[:, 256:] == 7).all()
+
+
 def test_scores_of_any_size(ctx):
     """A large scale, and scores that leave single keys: the running maximum moves far."""
     b = Batch("bf16", [900], [3], 4, 1, 64, seed=8)
