@@ -221,7 +221,11 @@ class Cache:
             raise ValueError(f"{name} is on {t.device}, k on {self.device}")
         if math.prod(shape) and not t[0].is_contiguous():
             raise ValueError(f"the pages of {name} must be contiguous")
-        return t.stride(0) if shape[0] > 1 else 0
+        if shape[0] <= 1:
+            return 0
+        if t.stride(0) < math.prod(shape[1:]):
+            raise ValueError(f"the pages of {name} overlap")
+        return t.stride(0)
 
     @classmethod
     def empty(cls, type, n_pages, Hkv, page, device=0):

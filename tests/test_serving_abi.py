@@ -4,6 +4,7 @@ documented codes before anything is launched."""
 import ctypes as ct
 import os
 import re
+import subprocess
 
 import pytest
 import torch
@@ -25,6 +26,36 @@ def test_symbols_and_structures():
     assert KV.mmi_rope_cfg.theta.offset == 32 and ct.sizeof(KV.mmi_rope_cfg) == 88
     assert KV.mmi_cache.page_stride.offset == 56 and ct.sizeof(KV.mmi_cache) == 72
     assert KV.mmi_tree.scale.offset == 128 and ct.sizeof(KV.mmi_tree) == 136
+
+
+def test_header_is_c(tmp_path):
+    """The header compiles as C99, and the compiler's structure sizes are the binding's."""
+    c = tmp_path / "sizes.c"
+    c.write_text('#include "mmi_cache.h"\n#include <stdio.h>\nint main(void) { printf("%zu %zu %zu", '
+                 'sizeof(mmi_rope_cfg), sizeof(mmi_cache), sizeof(mmi_tree)); return 0; }\n')
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), str(c), "-o",
+                    str(tmp_path / "sizes")], check=True, capture_output=True)
+    out = subprocess.run([str(tmp_path / "sizes")], check=True, capture_output=True, text=True).stdout.split()
+    assert [int(x) for x in out] == [ct.sizeof(s) for s in (KV.mmi_rope_cfg, KV.mmi_cache, KV.mmi_tree)]
+
+
+def test_rope_frequencies():
+    """mmi_rope_freq against the oracle, for every scaling."""
+    from oracle import serving as OS
+    for scaling, factor in (("none", 1.0), ("linear", 4.0), ("ntk", 8.0), ("parts", 16.0)):
+        for rot in (16, 96, 128):
+            kw = dict(theta=5e5, scaling=scaling, factor=factor, orig_len=8192.0, beta_fast=32.0, beta_slow=1.0)
+            cfg = KV.RopeCfg(rot_dim=rot, **kw)
+            got = [cfg.c[0].inv_freq[i] for i in range(rot // 2)]
+            assert all(abs(a - b) <= 2e-15 * b for a, b in zip(got, OS.frequencies(rot, **kw)))
+    L = KV.lib()
+    assert L.mmi_rope_freq(None, None) == INVALID
+    c = KV.mmi_rope_cfg(128, 0, 0, 0, (ct.c_int32 * 3)(0, 0, 0), 0, 10000.0, 1.0, 0.0, 32.0, 1.0, 0.0, None)
+    assert L.mmi_rope_freq(ct.byref(c), None) == INVALID
+    c.theta = -1.0
+    assert L.mmi_rope_freq(ct.byref(c), (ct.c_double * 64)()) == BAD_CONFIG
+    with pytest.raises(mmi.MMIError):
+        KV.RopeCfg(rot_dim=20)
 
 
 def rope(prob=None, cfg=None, q=DEV, k=DEV, qo=DEV, ko=DEV, pos=None, **kw):
@@ -158,6 +189,8 @@ def test_binding_refusals():
         KV.Cache("fp4", u8(3, 2, 16, 128), u8(3, 2, 16, 128), u8(3, 2, 16, 4), u8(3, 2, 16, 4))
     with pytest.raises(ValueError, match="contiguous"):
         KV.Cache("bf16", bf(3, 16, 2, 128).transpose(1, 2), bf(3, 16, 2, 128).transpose(1, 2))
+    with pytest.raises(ValueError, match="overlap"):
+        KV.Cache("bf16", bf(1, 2, 16, 128).expand(3, 2, 16, 128), bf(1, 2, 16, 128).expand(3, 2, 16, 128))
     with pytest.raises(ValueError, match="unknown"):
         KV.Cache("fp16", bf(3, 2, 16, 128), bf(3, 2, 16, 128))
     c = KV.Cache("bf16", bf(3, 2, 16, 128), bf(3, 2, 16, 128))
