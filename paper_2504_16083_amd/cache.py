@@ -213,6 +213,7 @@ class Cache:
         self.c = mmi_cache(TYPES[type], self.page, self.Hkv, D, self.n_pages, k.data_ptr(), v.data_ptr(),
                            None if bf16 else k_scale.data_ptr(), None if bf16 else v_scale.data_ptr(),
                            stride * (2 if bf16 else 1), scale)
+        self.ref = ct.byref(self.c)
 
     def _pool(self, name, t, dtype, shape):
         if t.dtype != dtype or tuple(t.shape) != shape:
@@ -250,7 +251,7 @@ def mmi_cache_write(ctx, cache, k, v, slot, stream=None):
     _on(ctx, cache)
     n = k.shape[0]
     ks, vs = _rows(ctx, "k", k, n, cache.Hkv), _rows(ctx, "v", v, n, cache.Hkv)
-    _check(lib().mmi_cache_write(ctx.h, ct.byref(cache.c), k.data_ptr(), *ks, v.data_ptr(), *vs,
+    _check(lib().mmi_cache_write(ctx.h, cache.ref, k.data_ptr(), *ks, v.data_ptr(), *vs,
                                  _array(ctx, "slot", slot, torch.int64, (n,)), n, _stream(ctx, stream)))
 
 
@@ -259,7 +260,7 @@ def mmi_cache_read(ctx, cache, slot, k, v, stream=None):
     _on(ctx, cache)
     n = k.shape[0]
     ks, vs = _rows(ctx, "k", k, n, cache.Hkv), _rows(ctx, "v", v, n, cache.Hkv)
-    _check(lib().mmi_cache_read(ctx.h, ct.byref(cache.c), _array(ctx, "slot", slot, torch.int64, (n,)), n,
+    _check(lib().mmi_cache_read(ctx.h, cache.ref, _array(ctx, "slot", slot, torch.int64, (n,)), n,
                                 k.data_ptr(), *ks, v.data_ptr(), *vs, _stream(ctx, stream)))
 
 
@@ -269,35 +270,50 @@ class Tree:
     [n_seq + 1], length int32 [n_seq] (cached tokens), pages int32 [n_seq,
     max_pages], mask int64 [n_rows, words] (bit j of a row: it sees drafted
     token j; None: token i sees 0 .. i), max_rows and max_len the most drafted
-    and cached tokens of a sequence. The tensors' contents may change between
-    calls, within these bounds."""
+    and cached tokens of a sequence. The tensors are checked once, here, and
+    stay the batch's; their contents may change between calls, within these
+    bounds, and so may max_rows, max_len and scale."""
 
     def __init__(self, row_start, length, pages, mask=None, max_rows=1, max_len=0, scale=0.0):
-        self.row_start, self.length, self.pages, self.mask = row_start, length, pages, mask
         self.max_rows, self.max_len, self.scale = max_rows, max_len, scale
+        self._tensors = row_start, length, pages, mask
+        self._n_seq, self.index = length.shape[0], length.get_device()
+        if pages.dim() != 2 or mask is not None and mask.dim() != 2:
+            raise ValueError("pages must be a tensor [n_seq, max_pages], mask one [n_rows, words]")
+        self._max_pages = pages.shape[1]
+        self._mask_rows, self._words = (None, 0) if mask is None else mask.shape
+        self._ptr = (self._array("row_start", row_start, torch.int32, (self._n_seq + 1,)),
+                     self._array("length", length, torch.int32, (self._n_seq,)),
+                     self._array("pages", pages, torch.int32, (self._n_seq, self._max_pages)),
+                     None if mask is None else self._array("mask", mask, torch.int64, tuple(mask.shape)))
 
-    def _struct(self, ctx, Hq, n_rows):
-        t = mmi_tree()
-        t.n_seq, t.n_rows, t.Hq, t.max_rows, t.max_len = self.length.shape[0], n_rows, Hq, self.max_rows, self.max_len
-        t.row_start = _array(ctx, "row_start", self.row_start, torch.int32, (t.n_seq + 1,))
-        t.length = _array(ctx, "length", self.length, torch.int32, (t.n_seq,))
-        if self.pages.dim() != 2:
-            raise ValueError("pages must be a tensor [n_seq, max_pages]")
-        t.max_pages = self.pages.shape[1]
-        t.pages = _array(ctx, "pages", self.pages, torch.int32, (t.n_seq, t.max_pages))
-        if self.mask is not None:
-            if self.mask.dim() != 2:
-                raise ValueError("mask must be a tensor [n_rows, words]")
-            t.mask_words = self.mask.shape[1]
-            t.mask = _array(ctx, "mask", self.mask, torch.int64, (n_rows, t.mask_words))
-        t.scale = self.scale
-        return t
+    row_start = property(lambda self: self._tensors[0])
+    length = property(lambda self: self._tensors[1])
+    pages = property(lambda self: self._tensors[2])
+    mask = property(lambda self: self._tensors[3])
+
+    def _array(self, name, t, dtype, shape):
+        if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape}")
+        if t.get_device() != self.index:
+            raise ValueError(f"{name} is on {t.device}, length on {self.length.device}")
+        return t.data_ptr()
+
+    def _struct(self, ctx, Hq, n_rows, *strides):
+        if self.index != ctx.device:
+            raise ValueError(f"the tree is on {self.length.device}, the context on device {ctx.device}")
+        if self._mask_rows is not None and self._mask_rows != n_rows:
+            raise ValueError(f"mask has {self._mask_rows} rows for {n_rows} of q")
+        if not strides:
+            strides = (0,) * 8
+        return mmi_tree(self._n_seq, n_rows, Hq, self.max_rows, self.max_len, self._max_pages, self._words, *self._ptr,
+                        *strides, self.scale)
 
 
 def mmi_tree_workspace(ctx, cache, tree, Hq, n_rows) -> int:
     """Bytes of workspace of a batch with these bounds."""
     need = ct.c_size_t()
-    _check(lib().mmi_tree_workspace(ctx.h, ct.byref(cache.c), ct.byref(tree._struct(ctx, Hq, n_rows)),
+    _check(lib().mmi_tree_workspace(ctx.h, cache.ref, ct.byref(tree._struct(ctx, Hq, n_rows)),
                                     ct.byref(need)))
     return need.value
 
@@ -311,12 +327,9 @@ def mmi_tree_attention(ctx, cache, tree, q, k, v, o, workspace, lse=None, stream
     n = q.shape[0]
     qs = _rows(ctx, "q", q, None, None)
     Hq = q.shape[1]
-    t = tree._struct(ctx, Hq, n)
-    t.q_stride_s, t.q_stride_h = qs
-    t.k_stride_s, t.k_stride_h = _rows(ctx, "k", k, n, cache.Hkv)
-    t.v_stride_s, t.v_stride_h = _rows(ctx, "v", v, n, cache.Hkv)
-    t.o_stride_s, t.o_stride_h = _rows(ctx, "o", o, n, Hq)
+    t = tree._struct(ctx, Hq, n, *qs, *_rows(ctx, "k", k, n, cache.Hkv), *_rows(ctx, "v", v, n, cache.Hkv),
+                     *_rows(ctx, "o", o, n, Hq))
     lp = None if lse is None else _array(ctx, "lse", lse, torch.float32, (Hq, n))
     wp = _array(ctx, "workspace", workspace, torch.uint8, (workspace.numel(),))
-    _check(lib().mmi_tree_attention(ctx.h, ct.byref(cache.c), ct.byref(t), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    _check(lib().mmi_tree_attention(ctx.h, cache.ref, ct.byref(t), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                     o.data_ptr(), lp, wp, workspace.numel(), _stream(ctx, stream)))

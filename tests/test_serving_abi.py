@@ -196,3 +196,28 @@ def test_binding_refusals():
     c = KV.Cache("bf16", bf(3, 2, 16, 128), bf(3, 2, 16, 128))
     with pytest.raises(ValueError, match="context"):
         KV.mmi_cache_write(_Ctx, c, bf(4, 2, 128), bf(4, 2, 128), torch.zeros(4, dtype=torch.int64))
+
+
+def test_tree_binding_refusals():
+    """A batch's tensors are checked when it is made, its device and rows with every call."""
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    mask = torch.zeros(5, 1, dtype=torch.int64)
+    for args in [(i32(2), i32(2), i32(2, 3)), (i32(3), i32(2).long(), i32(2, 3)), (i32(3), i32(2), i32(3, 3)),
+                 (i32(3), i32(2), i32(6)), (i32(3), i32(2), i32(3, 2).t()), (i32(6)[::2], i32(2), i32(2, 3)),
+                 (i32(3), i32(2), i32(2, 3), mask.int()), (i32(3), i32(2), i32(2, 3), mask[0])]:
+        with pytest.raises(ValueError, match="must be"):
+            KV.Tree(*args)
+    tree = KV.Tree(i32(3), i32(2), i32(2, 3), mask)
+    with pytest.raises(AttributeError):                      # another tensor is another batch
+        tree.length = i32(2)
+    with pytest.raises(ValueError, match="context"):
+        tree._struct(_Ctx, 4, 5)
+    host = type("", (), {"device": -1})
+    with pytest.raises(ValueError, match="5 rows for 4"):
+        tree._struct(host, 4, 4)
+    tree.max_rows, tree.max_len, tree.scale = 3, 48, 0.5
+    t = tree._struct(host, 4, 5, *range(8, 72, 8))
+    assert (t.n_seq, t.n_rows, t.Hq, t.max_rows, t.max_len, t.max_pages, t.mask_words) == (2, 5, 4, 3, 48, 3, 1)
+    assert (t.row_start, t.length, t.pages, t.mask) == tuple(x.data_ptr() for x in (tree.row_start, tree.length, tree.pages, mask))
+    assert [getattr(t, f"{x}_stride_{y}") for x in "qkvo" for y in "sh"] == list(range(8, 72, 8))
+    assert t.scale == 0.5 and t.reserved == 0
