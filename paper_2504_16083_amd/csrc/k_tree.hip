@@ -1040,34 +1040,50 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
   int not_all_finite = 0;
   if (it.chunk == it.chunks - 1) {
     const uint16_t* kb = (const uint16_t*)a.k.p + (int64_t)sq.row0 * a.k.ss + (int64_t)it.head * a.k.sh;
-    for (int d0 = 0; d0 < sq.T; d0 += SK) {
-      uint32_t seen[2 / WK];
+    // without a mask no row sees a token behind the tile's last
+    const int n = a.mask ? sq.T : min(sq.T, (it.tile * ROWS + ROWS - 1) / a.g + 1);
+    u32x4 kv[2], vv[2];
+    uint32_t seen[2 / WK], next_seen[2 / WK];
+    auto fetch = [&](int d0) INLINE {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int d = min(d0 + tid / 16 + 32 * i, sq.T - 1);
+        kv[i] = *reinterpret_cast<const u32x4*>(kb + (int64_t)d * a.k.ss + tid % 16 * 8);
+        vv[i] = *reinterpret_cast<const u32x4*>(vb + (int64_t)d * a.v.ss + tid % 16 * 8);
+      }
 #pragma unroll
       for (int x = 0; x < 2 / WK; ++x) {
         const int k0 = d0 + 32 * (wk + WK * x);
-        seen[x] = k0 < sq.T ? seen_drafts(a, sq, tok, k0) : 0u;
+        next_seen[x] = k0 < sq.T ? seen_drafts(a, sq, tok, k0) : 0u;
       }
-      int odd_here = 0;
+    };
+    // the next stage on its way while this one is attended, in two places in
+    // turn: one barrier a stage (64 sequences of 256 drafts and 400 cached
+    // tokens, no mask, 523 us for 563 with everything after one another)
+    fetch(0);
+    for (int d0 = 0; d0 < n; d0 += SK) {
+      Stage64& to = st[d0 / SK & 1];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int key = tid / 16 + 32 * i, d = min(d0 + key, sq.T - 1);
-        const u32x4 kv = *reinterpret_cast<const u32x4*>(kb + (int64_t)d * a.k.ss + tid % 16 * 8);
-        const u32x4 vv = *reinterpret_cast<const u32x4*>(vb + (int64_t)d * a.v.ss + tid % 16 * 8);
+        const int key = tid / 16 + 32 * i;
         u32x4 keep;
         const u32x4 none = {};
-        odd_here |= not_finite(vv, keep);
-        *reinterpret_cast<u32x4*>(&st[0].k[key * TK + tid % 16 * 8]) = kv;
-        *reinterpret_cast<u32x4*>(&st[0].v[key * TV + tid % 16 * 8]) = d0 + key < sq.T ? keep : none;
+        not_all_finite |= not_finite(vv[i], keep);
+        *reinterpret_cast<u32x4*>(&to.k[key * TK + tid % 16 * 8]) = kv[i];
+        *reinterpret_cast<u32x4*>(&to.v[key * TV + tid % 16 * 8]) = d0 + key < sq.T ? keep : none;
       }
-      not_all_finite |= __syncthreads_or(odd_here);
+#pragma unroll
+      for (int x = 0; x < 2 / WK; ++x) seen[x] = next_seen[x];
+      __syncthreads();
+      if (d0 + SK < n) fetch(d0 + SK);
 #pragma unroll
       for (int x = 0; x < 2 / WK; ++x) {
         const int sub = wk + WK * x;
-        if (active && d0 + 32 * sub < sq.T)
-          unit_alone(r, seen[x], a.sc, h, st[0].k + klane + 32 * sub * TK, st[0].v + vlane + 32 * sub * TV);
+        if (active && __any(seen[x] != 0))
+          unit_alone(r, seen[x], a.sc, h, to.k + klane + 32 * sub * TK, to.v + vlane + 32 * sub * TV);
       }
-      __syncthreads();
     }
+    not_all_finite = __syncthreads_or(not_all_finite);
   }
   if (steps > 0) {
     auto there = [&](int t) INLINE -> uint64_t {                  // keys of stage t that exist
@@ -1246,81 +1262,149 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
   }
 }
 
-// Joins the partials of the sequences that were cut into chunks. Workgroup
-// (row of a sequence's rows, KV head and sequence): 8 groups of 32 lanes take
-// every eighth partial, 4 channels a lane, JU of them in flight, and meet in
-// LDS.
-constexpr int JU = 4;
+// Joins the partials of the sequences that were cut into chunks. A workgroup
+// joins one of their rows after another (row, KV head, sequence): its waves
+// take every fourth partial, two channels a lane, JU of them in flight (the
+// statistics of those a lane each), and meet in LDS. Bound by latency, or with
+// many rows by reading the partials. The host does not know which sequences
+// were cut: with a workgroup for every row that may exist, 16 sequences of 128
+// drafts and 300 cached tokens took 87 us for 52 in all, 64 of 256 and 400
+// (28 heads on 4) 525 us for 290.
+constexpr int JU = 8;                 // a lane each of max8 and sum8
+constexpr int JOINS = 8;              // workgroups a compute unit
 
-template <int ROWS>
-__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a) {
-  const int rows = a.max_rows * a.g, row = blockIdx.x % rows;
-  const int head = blockIdx.x / rows % a.c.Hkv, b = blockIdx.x / rows / a.c.Hkv;
-  const Seq sq = sequence(a, b);
-  const int first = a.rec[2 * b], chunks = a.rec[2 * b + 1];
-  const int tok = row / a.g;
-  const int tiles = tiles_of<ROWS>(a, sq);
-  // A sequence without rows, or (row_start not ascending) behind the items that
-  // were launched, has no record: whatever the workspace held is no index.
-  if (tok >= sq.T || chunks <= 1 || first < 0 || first + (int64_t)chunks * a.c.Hkv * tiles > a.items) return;
-  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
-  const int64_t at0 = ((int64_t)first + (int64_t)head * tiles + row / ROWS) * ROWS + row % ROWS;
-  const int64_t step = (int64_t)a.c.Hkv * tiles * ROWS;        // from chunk to chunk
-  __shared__ float4 so[8][32], sml[8];
+struct JoinShared {
+  float2 o[4][64];
+  float m[4], lo[4], l[4];
+};
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+
+// Over eight neighbouring lanes: the other one of two, the other two of four,
+// and, those being alike, the mirrored of eight.
+__device__ __forceinline__ float max8(float x) {
+  x = fmaxf(x, dpp<0xb1>(x));
+  x = fmaxf(x, dpp<0x4e>(x));
+  return fmaxf(x, dpp<0x141>(x));
+}
+
+__device__ __forceinline__ float sum8(float x) {
+  x += dpp<0xb1>(x);
+  x += dpp<0x4e>(x);
+  return x + dpp<0x141>(x);
+}
+
+__device__ __forceinline__ void join_row(const TreeArgs& a, int64_t at0, int64_t step, int chunks, int64_t token,
+                                         int qh, JoinShared& sh) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float m = -INFINITY, l = 0.0f, lo = 0.0f;
-  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int p0 = grp; p0 < chunks; p0 += 8 * JU) {
-    float4 e[JU], y[JU];
-#pragma unroll
-    for (int u = 0; u < JU; ++u) {
-      const int64_t at = at0 + min(p0 + 8 * u, chunks - 1) * step;
-      e[u] = *reinterpret_cast<const float4*>(a.part_ml + at * 4);
-      y[u] = *reinterpret_cast<const float4*>(a.part_o + at * D + 4 * lane);
-    }
-    float mn = m;
+  float2 o = make_float2(0.0f, 0.0f);
+  for (int p0 = wave; p0 < chunks; p0 += 4 * JU) {
+    const int mine = p0 + 4 * (lane % JU);
+    const float4 e = *reinterpret_cast<const float4*>(a.part_ml + (at0 + min(mine, chunks - 1) * step) * 4);
+    float2 y[JU];
 #pragma unroll
     for (int u = 0; u < JU; ++u)
-      if (p0 + 8 * u < chunks) mn = fmaxf(mn, e[u].x);
+      y[u] = *reinterpret_cast<const float2*>(a.part_o + (at0 + min(p0 + 4 * u, chunks - 1) * step) * D + 2 * lane);
+    const bool there = mine < chunks;
+    const float mn = fmaxf(m, max8(there ? e.x : -INFINITY));
     const float f = m == -INFINITY ? 0.0f : fast_exp2(m - mn);
-    l *= f; lo *= f;
-    o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+    const float w = there && e.x != -INFINITY ? fast_exp2(e.x - mn) : 0.0f;
     m = mn;
+    lo = lo * f + sum8(there ? e.y * w : 0.0f);
+    l = l * f + sum8(there ? e.z * w : 0.0f);
+    o.x *= f; o.y *= f;
 #pragma unroll
     for (int u = 0; u < JU; ++u) {
-      if (p0 + 8 * u >= chunks) break;
-      const float w = e[u].x == -INFINITY ? 0.0f : fast_exp2(e[u].x - m);
-      lo += e[u].y * w;
-      l += e[u].z * w;
-      o.x += y[u].x * w; o.y += y[u].y * w; o.z += y[u].z * w; o.w += y[u].w * w;
+      if (p0 + 4 * u >= chunks) break;
+      const float wu = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), u));
+      o.x += y[u].x * wu; o.y += y[u].y * wu;
     }
   }
-  so[grp][lane] = o;
-  if (lane == 0) sml[grp] = make_float4(m, lo, l, 0.0f);
-  __syncthreads();
-  if (grp) return;
-  float4 part[8];
-#pragma unroll
-  for (int w = 0; w < 8; ++w) {
-    part[w] = sml[w];
-    m = fmaxf(m, part[w].x);
+  sh.o[wave][lane] = o;
+  if (lane == 0) {
+    sh.m[wave] = m;
+    sh.lo[wave] = lo;
+    sh.l[wave] = l;
   }
-  l = lo = 0.0f;
-  o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  __syncthreads();
+  if (wave) return;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) {
-    const float f = part[w].x == -INFINITY ? 0.0f : fast_exp2(part[w].x - m);
-    const float4 y = so[w][lane];
-    lo += part[w].y * f;
-    l += part[w].z * f;
-    o.x += y.x * f; o.y += y.y * f; o.z += y.z * f; o.w += y.w * f;
+  for (int x = 1; x < 4; ++x) m = fmaxf(m, sh.m[x]);
+  l = lo = 0.0f;
+  o = make_float2(0.0f, 0.0f);
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const float f = sh.m[x] == -INFINITY ? 0.0f : fast_exp2(sh.m[x] - m);
+    const float2 y = sh.o[x][lane];
+    lo += sh.lo[x] * f;
+    l += sh.l[x] * f;
+    o.x += y.x * f; o.y += y.y * f;
   }
   const float inv = lo > 0.0f ? 1.0f / lo : lo == 0.0f ? 0.0f : lo;
-  const int qh = head * a.g + row - tok * a.g;
-  uint16_t* to = a.o + (int64_t)(sq.row0 + tok) * a.o_ss + (int64_t)qh * a.o_sh + 4 * lane;
-  bf16x4 y = {(__bf16)(o.x * inv), (__bf16)(o.y * inv), (__bf16)(o.z * inv), (__bf16)(o.w * inv)};
-  *reinterpret_cast<bf16x4*>(to) = y;
-  if (a.lse && lane == 0)
-    a.lse[(int64_t)qh * a.n_rows + sq.row0 + tok] = l == 0.0f ? -INFINITY : (m + fast_log2(l)) * LN2;
+  const bf16e2 y = {(__bf16)(o.x * inv), (__bf16)(o.y * inv)};
+  *reinterpret_cast<bf16e2*>(a.o + token * a.o_ss + (int64_t)qh * a.o_sh + 2 * lane) = y;
+  if (a.lse && lane == 0) a.lse[(int64_t)qh * a.n_rows + token] = l == 0.0f ? -INFINITY : (m + fast_log2(l)) * LN2;
+}
+
+// A sequence without rows, or (row_start not ascending) behind the items that
+// were launched, has no record: whatever the workspace held is no index.
+__device__ __forceinline__ bool was_cut(const TreeArgs& a, const Seq& s, int first, int chunks, int tiles) {
+  return s.T > 0 && chunks > 1 && first >= 0 && first + (int64_t)chunks * a.c.Hkv * tiles <= a.items;
+}
+
+template <int ROWS>
+__device__ __forceinline__ void join_row_of(const TreeArgs& a, const Seq& s, int first, int chunks, int tiles, int at,
+                                            JoinShared& sh) {
+  const int rows = s.T * a.g, head = at / rows, row = at - head * rows, tok = row / a.g;
+  join_row(a, ((int64_t)first + (int64_t)head * tiles + row / ROWS) * ROWS + row % ROWS, (int64_t)a.c.Hkv * tiles * ROWS,
+           chunks, s.row0 + tok, head * a.g + row - tok * a.g, sh);
+}
+
+// EACH: a workgroup for every row that may exist. Few as they are, a workgroup
+// then has nothing to search for (64 drafts over 8192 tokens 35.9 us for 37.2).
+template <int ROWS, bool EACH>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(JOINS))) void k_tree_join(TreeArgs a) {
+  __shared__ JoinShared sh;
+  if constexpr (EACH) {
+    const int most = a.max_rows * a.g * a.c.Hkv, b = blockIdx.x / most, at = blockIdx.x - b * most;
+    const Seq s = sequence(a, b);
+    const int first = a.rec[2 * b], chunks = a.rec[2 * b + 1], tiles = tiles_of<ROWS>(a, s);
+    if (was_cut(a, s, first, chunks, tiles) && at < s.T * a.g * a.c.Hkv)
+      join_row_of<ROWS>(a, s, first, chunks, tiles, at, sh);
+    return;
+  }
+  int next = blockIdx.x, base = 0;                         // this workgroup's next row; rows of the sequences before
+  for (int b0 = 0; b0 < a.n_seq; b0 += 64) {               // a sequence a lane, in every wave
+    const int lane = threadIdx.x & 63, b = b0 + lane;
+    Seq s = {0, 0, 0};
+    int first = 0, chunks = 0;
+    if (b < a.n_seq) {
+      s = sequence(a, b);
+      first = a.rec[2 * b];
+      chunks = a.rec[2 * b + 1];
+    }
+    const int tiles = tiles_of<ROWS>(a, s);
+    const int n = was_cut(a, s, first, chunks, tiles) ? s.T * a.g * a.c.Hkv : 0;   // host: below 2^23 of all sequences
+    int end = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(end, d);
+      if (lane >= d) end += y;
+    }
+    const int all = __builtin_amdgcn_readlane(end, 63);
+    for (; next < base + all; next += gridDim.x) {
+      const int at = next - base, l = __builtin_ctzll(__ballot(at >= end - n && at < end));
+      auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+      const Seq sl = {of(s.row0), of(s.T), of(s.L)};
+      join_row_of<ROWS>(a, sl, of(first), of(chunks), of(tiles), at - of(end - n), sh);
+      __syncthreads();
+    }
+    base += all;
+  }
 }
 
 TreeShape tree_shape(const mmi_tree& t, int Hkv, int type, int cus) {
@@ -1360,6 +1444,14 @@ static void launch_type(const TreeArgs& a, int rows, hipStream_t st) {
   else hipLaunchKernelGGL((k_tree_wide<TYPE, 8, false>), grid, dim3(NTW), 0, st, a);
 }
 
+template <int ROWS>
+static void launch_join(const TreeArgs& a, hipStream_t st) {
+  // rows of the largest batch within the bounds (below 2^23), and as many workgroups as run at once
+  const int64_t rows = (int64_t)a.max_rows * a.n_seq * a.g * a.c.Hkv, most = JOINS * (int64_t)a.cus;
+  if (rows <= most) hipLaunchKernelGGL((k_tree_join<ROWS, true>), dim3((unsigned)rows), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_tree_join<ROWS, false>), dim3((unsigned)most), dim3(256), 0, st, a);
+}
+
 hipError_t launch_tree(const TreeArgs& a, int type, int rows, hipStream_t st) {
   if (a.n_seq <= 0 || a.n_rows <= 0) return hipSuccess;
   switch (type) {
@@ -1371,11 +1463,12 @@ hipError_t launch_tree(const TreeArgs& a, int type, int rows, hipStream_t st) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.max_len <= CHUNK) return e;   // one chunk a sequence at most
-  const dim3 join((unsigned)(a.max_rows * a.g * a.c.Hkv * a.n_seq));
-  if (rows == 16) hipLaunchKernelGGL(k_tree_join<16>, join, dim3(256), 0, st, a);
-  else if (rows == 32) hipLaunchKernelGGL(k_tree_join<32>, join, dim3(256), 0, st, a);
-  else if (rows == 128) hipLaunchKernelGGL(k_tree_join<128>, join, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_tree_join<256>, join, dim3(256), 0, st, a);
+  switch (rows) {
+    case 16: launch_join<16>(a, st); break;
+    case 32: launch_join<32>(a, st); break;
+    case 128: launch_join<128>(a, st); break;
+    default: launch_join<256>(a, st);
+  }
   return hipGetLastError();
 }
 

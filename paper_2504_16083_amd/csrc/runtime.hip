@@ -1686,6 +1686,7 @@ int mmi_tree_attention(mmi_ctx* ctx, const mmi_cache* cache, const mmi_tree* tre
     a.part_ml = reinterpret_cast<float*>(ws + s.part_ml);
     a.rec = reinterpret_cast<int32_t*>(ws + s.rec);
     a.target = s.target;
+    a.cus = ctx->cus;
     a.items = s.items;
     OnDevice d(ctx->device);
     HIPCHK(launch_tree(a, cache->type, s.rows, (hipStream_t)stream));
