@@ -56,6 +56,18 @@ def test_many_sequences(ctx):
     b.check(o, lse, rows={(s, i) for s in [0, 1, 2, 3, 4, 5, 254, 255, 256, 257, 300, 511, 512, 598, 599] for i in (0, 1)})
 
 
+@pytest.mark.parametrize("n,T", [(140, 2), (140, 5), (9, 40)])
+def test_joined_rows(ctx, n, T):
+    """More rows than workgroups that join them, some of sequences in one piece between those that were cut."""
+    rng = np.random.default_rng(T)
+    long = sorted({0, 3, 63, 64, 65, 127, 128, n - 1} & set(range(n)))
+    lens = [700 + 11 * b if b in long else int(rng.integers(0, 100)) for b in range(n)]
+    drafts = [T if b in long else int(rng.integers(0, T + 1)) for b in range(n)]
+    b = Batch("int8", lens, drafts, 8, 1, 16, seed=n, mask="tree")
+    o, lse = b.run(ctx)
+    b.check(o, lse, rows={(s, i) for s in [*long, 1, 2, n // 2] for i in (0, T - 1)})
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("T,g", [(1, 7), (6, 8), (16, 7), (40, 7)])
 def test_long_cache(ctx, kind, T, g):
