@@ -1309,6 +1309,12 @@ __device__ __forceinline__ void join_row(const TreeArgs& a, int64_t at0, int64_t
 #pragma unroll
     for (int u = 0; u < JU; ++u)
       y[u] = *reinterpret_cast<const float2*>(a.part_o + (at0 + min(p0 + 4 * u, chunks - 1) * step) * D + 2 * lane);
+    // used here: the compiler would load each where it is added, one after another
+#pragma unroll
+    for (int u = 0; u < JU; ++u) {
+      pin(y[u].x);
+      pin(y[u].y);
+    }
     const bool there = mine < chunks;
     const float mn = fmaxf(m, max8(there ? e.x : -INFINITY));
     const float f = m == -INFINITY ? 0.0f : fast_exp2(m - mn);
