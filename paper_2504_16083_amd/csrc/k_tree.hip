@@ -578,44 +578,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
     load_block<TYPE>(raw, a, pid, it.head, t0, it.c1, lane);
     block_pages(pid, a, pages, t0 + 4 * KB, it.c1, zero);
   }
-  // The drafted tokens come first: the loads of the first block are on their
-  // way meanwhile (8 sequences of 8 drafts over 3000 tokens 28.8 us for 29.9
-  // with the drafted tokens last).
-  const uint16_t* vb = (const uint16_t*)a.v.p + (int64_t)sq.row0 * a.v.ss + (int64_t)it.head * a.v.sh;
-  uint64_t odd = 0;
-  if (it.chunk == it.chunks - 1) {
-    const uint16_t* kb = (const uint16_t*)a.k.p + (int64_t)sq.row0 * a.k.ss + (int64_t)it.head * a.k.sh;
-    for (int d0 = KB * wave; d0 < sq.T; d0 += 4 * KB) {
-      uint32_t seen[RN];
-#pragma unroll
-      for (int n = 0; n < RN; ++n) seen[n] = seen_drafts(a, sq, tok[n], d0);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int key = 4 * i + lane / 16;
-        const u32x4 raw_v = *reinterpret_cast<const u32x4*>(vb + (int64_t)min(d0 + key, sq.T - 1) * a.v.ss + lane % 16 * 8);
-        u32x4 keep;
-        const u32x4 none = {};
-        odd |= __ballot(not_finite(raw_v, keep));
-        *reinterpret_cast<u32x4*>(v + key * TV + lane % 16 * 8) = d0 + key < sq.T ? keep : none;
-      }
-      f32x4 s[RN][2];
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const uint16_t* kp = kb + (int64_t)min(d0 + 16 * half + c, sq.T - 1) * a.k.ss;
-#pragma unroll
-        for (int n = 0; n < RN; ++n) s[n][half] = f32x4{};
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const bf16x8 op = load16(kp + channel<TYPE>(x, q));
-#pragma unroll
-          for (int n = 0; n < RN; ++n) s[n][half] = mfma16(op, r.q[n][x], s[n][half]);
-        }
-      }
-      wave_fence();
-      attend_few<RN>(r, s, v, seen, a.sc, q, vlane);
-      wave_fence();
-    }
-  }
   for (; t0 < it.c1; t0 += 4 * KB) {
     uint32_t seen[RN];
 #pragma unroll
@@ -641,13 +603,42 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
     attend_few<RN>(r, s, v, seen, a.sc, q, vlane);
     wave_fence();
   }
-  if (odd)                                                 // at the end: nothing scales what these put into O
+  if (it.chunk == it.chunks - 1) {
+    const uint16_t* kb = (const uint16_t*)a.k.p + (int64_t)sq.row0 * a.k.ss + (int64_t)it.head * a.k.sh;
+    const uint16_t* vb = (const uint16_t*)a.v.p + (int64_t)sq.row0 * a.v.ss + (int64_t)it.head * a.v.sh;
     for (int d0 = KB * wave; d0 < sq.T; d0 += 4 * KB) {
+      uint64_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = 4 * i + lane / 16;
+        const u32x4 raw_v = *reinterpret_cast<const u32x4*>(vb + (int64_t)min(d0 + key, sq.T - 1) * a.v.ss + lane % 16 * 8);
+        u32x4 keep;
+        const u32x4 none = {};
+        odd |= __ballot(not_finite(raw_v, keep));
+        *reinterpret_cast<u32x4*>(v + key * TV + lane % 16 * 8) = d0 + key < sq.T ? keep : none;
+      }
+      f32x4 s[RN][2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const uint16_t* kp = kb + (int64_t)min(d0 + 16 * half + c, sq.T - 1) * a.k.ss;
+#pragma unroll
+        for (int n = 0; n < RN; ++n) s[n][half] = f32x4{};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const bf16x8 op = load16(kp + channel<TYPE>(x, q));
+#pragma unroll
+          for (int n = 0; n < RN; ++n) s[n][half] = mfma16(op, r.q[n][x], s[n][half]);
+        }
+      }
       uint32_t seen[RN];
 #pragma unroll
       for (int n = 0; n < RN; ++n) seen[n] = seen_drafts(a, sq, tok[n], d0);
-      add_not_finite_few<RN>(r, v, vb + (int64_t)d0 * a.v.ss, a.v.ss, sq.T - d0, seen, q, vlane, lane);
+      wave_fence();
+      attend_few<RN>(r, s, v, seen, a.sc, q, vlane);
+      wave_fence();
+      if (odd) add_not_finite_few<RN>(r, v, vb + (int64_t)d0 * a.v.ss, a.v.ss, sq.T - d0, seen, q, vlane, lane);
     }
+  }
 
   // the waves' parts of each row, weighed by their maxima
 #pragma unroll
