@@ -287,10 +287,14 @@ class Tree:
                      self._array("pages", pages, torch.int32, (self._n_seq, self._max_pages)),
                      None if mask is None else self._array("mask", mask, torch.int64, tuple(mask.shape)))
 
-    row_start = property(lambda self: self._tensors[0])
-    length = property(lambda self: self._tensors[1])
-    pages = property(lambda self: self._tensors[2])
-    mask = property(lambda self: self._tensors[3])
+    def _held(i):
+        def same(self, t):                         # tree.length += 1 ends here with the tensor itself
+            if t is not self._tensors[i]:
+                raise AttributeError("a batch keeps its tensors; make another Tree for others")
+        return property(lambda self: self._tensors[i], same)
+
+    row_start, length, pages, mask = _held(0), _held(1), _held(2), _held(3)
+    del _held
 
     def _array(self, name, t, dtype, shape):
         if t.dtype != dtype or t.shape != shape or not t.is_contiguous():

@@ -210,6 +210,8 @@ def test_tree_binding_refusals():
     tree = KV.Tree(i32(3), i32(2), i32(2, 3), mask)
     with pytest.raises(AttributeError):                      # another tensor is another batch
         tree.length = i32(2)
+    tree.length += 1                                         # its contents are the caller's
+    assert tree.length.tolist() == [1, 1]
     with pytest.raises(ValueError, match="context"):
         tree._struct(_Ctx, 4, 5)
     host = type("", (), {"device": -1})
