@@ -153,8 +153,9 @@ typedef struct mmi_tree {
 int mmi_tree_workspace(mmi_ctx* ctx, const mmi_cache* cache, const mmi_tree* tree, size_t* bytes);
 
 /* o [n_rows, Hq, 128] = softmax(scale q k^T) v over the keys that a row sees,
- * scores and softmax in fp32, P rounded to bfloat16 for the product with V,
- * o rounded once; lse: device float [Hq][n_rows] natural-log sums, or NULL. A
+ * scores and softmax in fp32; the weights enter the product with V in 15 bits
+ * up to 32 rows a KV head (max_rows * Hq / Hkv), with more rounded to bfloat16
+ * (8 bits); o rounded once; lse: device float [Hq][n_rows] natural-log sums, or NULL. A
  * row that sees no key gets o = 0 and lse = -inf. A drafted token that a row
  * does not see has no part in it, whatever its K and V hold (infinities and
  * NaN too). Query head h reads KV head h / (Hq / Hkv). o must not overlap an

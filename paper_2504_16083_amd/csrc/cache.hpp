@@ -56,8 +56,8 @@ struct TreeArgs {
   int32_t target;                  // workgroups that a batch is cut into, if it is long enough
   int32_t items;                   // launched workgroups = partials the workspace holds
   int32_t cus;                     // compute units
-  float* part_o;                   // [items][rows of a tile][128], sums over the bf16 P
-  float* part_ml;                  // [items][rows of a tile][4]: maximum (log2 units), bf16-P sum, fp32-P sum
+  float* part_o;                   // [items][rows of a tile][128], sums over P as it entered the product
+  float* part_ml;                  // [items][rows of a tile][4]: maximum (log2 units), sum of that P, fp32-P sum
   int32_t* rec;                    // [n_seq][2]: a sequence's first item and the chunks of its keys
 };
 struct TreeShape {                 // how a batch is cut, from its bounds alone

@@ -437,7 +437,7 @@ template <int RN>
 struct FewRows {                       // a wave's RN tiles of 16 rows
   f32x4 o[RN][8];
   bf16x8 q[RN][4];
-  float m[RN], l[RN], lo[RN];          // maximum (log2 units) of a row; sums of this lane's P (fp32, bf16)
+  float m[RN], l[RN];                  // maximum (log2 units) of a row; sum of this lane's P
 };
 
 __device__ __forceinline__ float group_max(float x) {   // over the four lane groups
@@ -456,10 +456,18 @@ __device__ __forceinline__ bf16x8 v_operand16(const uint16_t* v, int vlane, int 
 
 // Scores of the block (s[n][half]: keys 16 half + 4 q + i) and the staged V
 // against the wave's rows; bit k of seen[n]: this lane's row sees key k.
+// P enters the product in two bfloat16 pieces that hold 15 bits of it: its
+// first 8 bits, cut, and what is left plus 2^-17 of it (in all weights alike;
+// without it the rest might be 0, and meet an infinity in V). Rounded to one
+// piece, O was off by up to 2^-8 of the spread of V. The matrix cores have
+// the time, the vector ALU has it but for the small types: one token over
+// 524288, 32 heads on 8, bfloat16 365 us for 364 with one piece, E4M3 200 for
+// 200, int8 229 for 224, E2M1 121 for 115; 4 drafts of 7 heads a KV head over
+// 262144 125 for 124, 59 for 58, 80 for 75 and 52 for 47.
 template <int RN>
 __device__ __forceinline__ void attend_few(FewRows<RN>& r, f32x4 (&s)[RN][2], const uint16_t* v,
                                            const uint32_t (&seen)[RN], float sc, int q, int vlane) {
-  bf16x8 p[RN];
+  bf16x8 p[RN], rest[RN];
 #pragma unroll
   for (int n = 0; n < RN; ++n) {
     if (__any(seen[n] != 0xffffffffu)) {
@@ -476,29 +484,26 @@ __device__ __forceinline__ void attend_few(FewRows<RN>& r, f32x4 (&s)[RN][2], co
       const float m = fmaxf(r.m[n], mx), alpha = r.m[n] == m ? 1.0f : fast_exp2(r.m[n] - m);
       r.m[n] = m;
       r.l[n] *= alpha;
-      r.lo[n] *= alpha;
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
         for (int x = 0; x < 4; ++x) r.o[n][dt][x] *= alpha;
     }
     const float base = r.m[n] == -INFINITY ? 0.0f : r.m[n];   // nothing seen yet: every P is 2^-inf = 0
-    const bf16e2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
       const float e = fast_exp2(fmaf(s[n][x >> 2][x & 3], sc, -base));
       r.l[n] += e;
-      p[n][x] = (__bf16)e;                   // rounded for the product; O is divided by the sum of these
+      const uint32_t top = __float_as_uint(e) & 0xffff0000u;
+      p[n][x] = __builtin_bit_cast(__bf16, (uint16_t)(top >> 16));
+      rest[n][x] = (__bf16)fmaf(e, 1.0f + 0x1p-17f, -__uint_as_float(top));
     }
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-      r.lo[n] = __builtin_amdgcn_fdot2_f32_bf16(bf16e2{p[n][2 * x], p[n][2 * x + 1]}, one, r.lo[n], false);
   }
 #pragma unroll
   for (int dt = 0; dt < 8; ++dt) {
     const bf16x8 av = v_operand16(v, vlane, dt);
 #pragma unroll
-    for (int n = 0; n < RN; ++n) r.o[n][dt] = mfma16(av, p[n], r.o[n][dt]);
+    for (int n = 0; n < RN; ++n) r.o[n][dt] = mfma16(av, rest[n], mfma16(av, p[n], r.o[n][dt]));
   }
 }
 
@@ -536,7 +541,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
   // V blocks of the four waves; at the end their O, a tile of 16 rows at a time
   __shared__ __align__(16) uint16_t vs[4 * KB * TV];
   static_assert(sizeof(vs) >= 4 * 16 * OP * sizeof(float), "the join buffer lies in the V blocks");
-  __shared__ float ml[4][ROWS][4];
+  __shared__ __align__(8) float ml[4][ROWS][2];
   __shared__ int64_t sh64[4];
   __shared__ int sh[8];
   Item it;
@@ -567,7 +572,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) r.o[n][dt] = f32x4{};
     r.m[n] = -INFINITY;
-    r.l[n] = r.lo[n] = 0.0f;
+    r.l[n] = 0.0f;
   }
 
   const int32_t* pages = a.pages + (int64_t)it.b * a.max_pages;
@@ -647,9 +652,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
   for (int n = 0; n < RN; ++n) {
     r.l[n] += __shfl_xor(r.l[n], 16);
     r.l[n] += __shfl_xor(r.l[n], 32);
-    r.lo[n] += __shfl_xor(r.lo[n], 16);
-    r.lo[n] += __shfl_xor(r.lo[n], 32);
-    if (q == 0) *reinterpret_cast<float4*>(ml[wave][16 * n + c]) = make_float4(r.m[n], r.lo[n], r.l[n], 0.0f);
+    if (q == 0) *reinterpret_cast<float2*>(ml[wave][16 * n + c]) = make_float2(r.m[n], r.l[n]);
   }
 #pragma unroll
   for (int n = 0; n < RN; ++n) {
@@ -669,18 +672,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
     const int jr = tid >> 4, part = tid & 15;              // row of the tile, 8 channels
     const int row = it.tile * ROWS + 16 * n + jr, jtok = row / a.g;
     if (jtok >= sq.T) continue;
-    const float (*mr)[ROWS][4] = ml;
+    const float (*mr)[ROWS][2] = ml;
     float m = mr[0][16 * n + jr][0];
 #pragma unroll
     for (int w = 1; w < 4; ++w) m = fmaxf(m, mr[w][16 * n + jr][0]);
-    float l = 0.0f, lo = 0.0f, o[8];
+    float l = 0.0f, o[8];
 #pragma unroll
     for (int x = 0; x < 8; ++x) o[x] = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       const float wm = mr[w][16 * n + jr][0], f = wm == -INFINITY ? 0.0f : fast_exp2(wm - m);
-      lo += mr[w][16 * n + jr][1] * f;
-      l += mr[w][16 * n + jr][2] * f;
+      l += mr[w][16 * n + jr][1] * f;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(vs) + (w * 16 + jr) * OP +
@@ -689,7 +691,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
       }
     }
     if (it.chunks == 1) {
-      const float inv = lo > 0.0f ? 1.0f / lo : lo == 0.0f ? 0.0f : lo;   // no key seen: 0; NaN stays
+      const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;       // no key seen: 0; NaN stays
       const int head = it.head * a.g + row - jtok * a.g;
       bf16x8 y;
 #pragma unroll
@@ -702,7 +704,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
       float* to = a.part_o + at * D + part * 8;
       *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
       *reinterpret_cast<float4*>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
-      if (part == 0) *reinterpret_cast<float4*>(a.part_ml + at * 4) = make_float4(m, lo, l, 0.0f);
+      if (part == 0) *reinterpret_cast<float4*>(a.part_ml + at * 4) = make_float4(m, l, l, 0.0f);
     }
   }
 }
@@ -858,6 +860,12 @@ __device__ __forceinline__ void pin(T& x) { asm volatile("" : "+v"(x)); }
 // a unit's maxima first put 20 dependent instructions before the exponentials
 // of every slot: six ragged trees 402 us for 383, 16 drafts over 1M tokens in
 // four bits 451 for 425.)
+// P is rounded to bfloat16 for the product and O divided by the sum of the
+// rounded, so that only the roundings' scatter is left: each weight is off by
+// up to 2^-8, the mean of many by less. P in two pieces as with few rows makes
+// a slot's 16 MFMAs 24: 64 drafts over 131072, 28 heads on 4, bfloat16 243 us
+// for 173, 16 over 1048576 in E2M1 485 for 378, 256 of 64 sequences over 400 in
+// E4M3 345 for 295.
 constexpr int PIECES = 18;
 constexpr float MOST = 4096.0f;
 struct SoftState {

@@ -319,3 +319,28 @@ def test_prefill_then_decode(ctx, kind):
     place = torch.where(keep >= 0, pages.long()[torch.clamp(keep, 0, len(pages) * page - 1) // page] * page + keep % page, -1)
     KV.mmi_cache_write(ctx, cache, k[n:], v[n:], place)
     assert int((cache.k != before).flatten(3).any(-1).any(1).sum()) == sum(1 for j in range(0, T, 2))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("T,g", [(1, 7), (2, 16)])
+@pytest.mark.parametrize("L", [6, 33, 300, 3000])
+def test_weights_of_few_rows_keep_15_bits(ctx, kind, T, g, L):
+    """Up to 32 rows a head a weight enters the product with V in two bfloat16 pieces: it is off by half a step of
+    the second, 2^-8 of what the first, cut after 8 bits, has left (2^-15), and the 2^-17 that it is given more.
+    Exponentials and the scores' rounding as in compare(); n terms in fp32 lose n 2^-24 of the sums at most. All of
+    it acts on weights times |v|, whose mean is at most |o| + spread."""
+    from oracle import serving as OS
+    from serving import HALF_STEP, score_error
+    b = Batch(kind, [L], [T], g, 1, 64, seed=L + T)
+    got, q, k, v = f64(b.run(ctx, lse=False)[0]), f64(b.q), f64(b.k), f64(b.v)
+    kk, vv = np.concatenate([b.K[b.slots[0], 0], k[:, 0]]), np.concatenate([b.V[b.slots[0], 0], v[:, 0]])
+    worst = 0.0
+    for i in range(T):
+        sees = np.concatenate([np.ones(L, bool), b.sees[0][i]])
+        for x in range(g):
+            want, _, spread, bound = OS.attend(q[i, x], kk, vv, sees, b.scale)
+            part = 2.0 ** -15 + 2.0 ** -17 + 2 * score_error(bound) + 2.0 ** -20 + len(sees) * 2.0 ** -24
+            tol = (np.abs(want) + spread) * part
+            tol = tol * (1 + HALF_STEP) + HALF_STEP * np.abs(want) + 1e-30
+            worst = max(worst, (np.abs(got[i, x] - want) / tol).max())
+    assert worst <= 1, worst
