@@ -187,7 +187,7 @@ mmi_tree tree_checked(const mmi_cache* c, const mmi_tree* tree) {
   if (t.max_rows < 1) fail(MMI_ERR_INVALID_ARG, "max_rows must be >= 1");
   if (t.max_rows > 256) fail(MMI_ERR_UNSUPPORTED, "more than 256 drafted tokens of a sequence");
   if (t.max_len < 0) fail(MMI_ERR_INVALID_ARG, "max_len is negative");
-  if (t.max_len > (1 << 30)) fail(MMI_ERR_UNSUPPORTED, "max_len exceeds 2^30");
+  if (t.max_len > LONGEST) fail(MMI_ERR_UNSUPPORTED, "max_len exceeds 2^30");
   if (t.max_pages < 0 || (int64_t)t.max_pages * c->page < t.max_len)
     fail(MMI_ERR_INVALID_ARG, "max_pages pages of %d tokens do not hold max_len", c->page);
   if (t.mask && t.mask_words < (t.max_rows + 63) / 64)

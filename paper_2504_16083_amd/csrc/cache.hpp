@@ -68,6 +68,41 @@ struct TreeShape {                 // how a batch is cut, from its bounds alone
 TreeShape tree_shape(const mmi_tree& t, int Hkv, int type, int cus);
 hipError_t launch_tree(const TreeArgs& a, int type, int rows, hipStream_t st);
 
+// How the device cuts a batch. The chunk length follows from the work of the
+// whole batch (cached tokens x tiles x heads, cut into `target` parts), so long
+// sequences get many chunks and short ones few, whatever the bounds were. The
+// last chunks are shorter than the others, so that there are more items than
+// parts; as `target` of them run at once, the chunks are then made longer
+// until all start together (a second round of a few items takes as long as
+// the first: a ragged batch of 32 decoded tokens took 74 us for 65).
+constexpr int CHUNK = 128;         // chunks are multiples of a step of the four waves
+constexpr int64_t LONGEST = 1 << 30;   // cached tokens a sequence, and so a chunk: a multiple of CHUNK
+
+// No chunk is longer than a sequence may be: work / parts alone can be the
+// tokens of all sequences, more than 31 bits hold.
+__host__ __device__ inline int chunk_of(int64_t work, int64_t parts) {
+  const int64_t len = work < (1 << 30) ? ((int)work + (int)parts - 1) / (int)parts : (work + parts - 1) / parts;
+  return ((int)(len < 1 ? 1 : len < LONGEST ? len : LONGEST) + CHUNK - 1) / CHUNK * CHUNK;
+}
+
+// Chunks of a sequence of L tokens; the sum stays below 2^31.
+__host__ __device__ inline int chunks_of(int L, int chunk) { return L > chunk ? (L + chunk - 1) / chunk : 1; }
+
+// Chunk of a batch with this work (cached tokens x tiles) and these tiles;
+// count(chunk): its tiles x chunks.
+template <typename F>
+__host__ __device__ inline int choose_chunk(int64_t work, int64_t tiles, int Hkv, int target, F&& count) {
+  work *= Hkv;
+  const int chunk = chunk_of(work, target);
+  const int64_t items = count(chunk) * Hkv, units = tiles * Hkv;
+  if (items <= target || units >= target) return chunk;
+  // at most units + work / chunk items: the second length always fits
+  const int64_t fewer = target * (int64_t)target / items;
+  const int longer = chunk_of(work, fewer > 1 ? fewer : 1);
+  const int safe = chunk_of(work, target - units);
+  return longer < safe && count(longer) * Hkv <= target ? longer : safe;
+}
+
 // ---------------------------------------------------------------- cache.hip
 // Host checks (they throw Error) and the records for the launches.
 double rope_freq(const mmi_rope_cfg* cfg, double* freq);

@@ -26,7 +26,6 @@ constexpr int KB = 32;                 // keys of a block
 constexpr int TK = 136, TV = 160;      // bf16 a staged K / V row: operand reads without bank conflicts
 constexpr int OP = 132;                // floats a row of the join buffer
 constexpr float SLACK = 8.0f;          // the maximum moves when a block's passes it by this (log2 units)
-constexpr int CHUNK = 128;             // chunks are multiples of a step of the four waves
 
 typedef __attribute__((address_space(3))) bf16x4 lds4;
 
@@ -80,34 +79,8 @@ struct Item {
   Seq seq;
 };
 
-// Item `it` of the batch. The chunk length follows from the work of the whole
-// batch (cached tokens x tiles x heads, cut into `target` parts), so long
-// sequences get many chunks and short ones few, whatever the bounds were. The
-// last chunks are shorter than the others, so that there are more items than
-// parts; as `target` of them run at once, the chunks are then made longer
-// until all start together (a second round of a few items takes as long as
-// the first: a ragged batch of 32 decoded tokens took 74 us for 65).
-__device__ __forceinline__ int chunk_of(int64_t work, int64_t parts) {
-  const int64_t len = work < (1 << 30) ? ((int)work + (int)parts - 1) / (int)parts : (work + parts - 1) / parts;
-  return (int)((max(len, (int64_t)1) + CHUNK - 1) / CHUNK * CHUNK);
-}
-
 template <int ROWS>
 __device__ __forceinline__ int tiles_of(const TreeArgs& a, const Seq& s) { return (s.T * a.g + ROWS - 1) / ROWS; }
-
-// Chunk of a batch with this work (cached tokens x tiles) and these tiles;
-// count(chunk): its tiles x chunks.
-template <typename F>
-__device__ __forceinline__ int choose_chunk(const TreeArgs& a, int64_t work, int64_t tiles, F&& count) {
-  work *= a.c.Hkv;
-  const int chunk = chunk_of(work, a.target);
-  const int64_t items = count(chunk) * a.c.Hkv, units = tiles * a.c.Hkv;
-  if (items <= a.target || units >= a.target) return chunk;
-  // at most units + work / chunk items: the second length always fits
-  const int longer = chunk_of(work, max((int64_t)1, a.target * (int64_t)a.target / items));
-  const int safe = chunk_of(work, a.target - units);
-  return longer < safe && count(longer) * a.c.Hkv <= a.target ? longer : safe;
-}
 
 __device__ __forceinline__ void set_item(const TreeArgs& a, Item& r, int it, int b, int first, int tiles, int chunk,
                                          const Seq& s) {
@@ -115,7 +88,7 @@ __device__ __forceinline__ void set_item(const TreeArgs& a, Item& r, int it, int
   r.b = b;
   r.first = first;
   r.seq = s;
-  r.chunks = max(1, (s.L + chunk - 1) / chunk);
+  r.chunks = chunks_of(s.L, chunk);
   r.chunk = at / (tiles * a.c.Hkv);
   const int rest = at - r.chunk * tiles * a.c.Hkv;
   r.head = rest / tiles;
@@ -130,16 +103,16 @@ __device__ __forceinline__ int wave_sum(int x) {
   return x;
 }
 
-// Up to 64 sequences every wave finds the item by itself, a sequence a lane;
-// more are scanned by the workgroup, NT at a time.
+// Item `it` of the batch. Up to 64 sequences every wave finds it by itself, a
+// sequence a lane; more are scanned by the workgroup, NT at a time.
 template <int ROWS, int NT>
 __device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, int64_t* sh64, int* sh) {
   const int tid = threadIdx.x;
   if (a.n_seq == 1) {
     const Seq s = sequence(a, 0);
     const int tiles = tiles_of<ROWS>(a, s);
-    auto count = [&](int chunk) -> int64_t { return (int64_t)tiles * max(1, (s.L + chunk - 1) / chunk); };
-    const int chunk = choose_chunk(a, (int64_t)tiles * s.L, tiles, count);
+    auto count = [&](int chunk) -> int64_t { return (int64_t)tiles * chunks_of(s.L, chunk); };
+    const int chunk = choose_chunk((int64_t)tiles * s.L, tiles, a.c.Hkv, a.target, count);
     if (it >= count(chunk) * a.c.Hkv) return false;
     set_item(a, r, it, 0, 0, tiles, chunk, s);
   } else if (a.n_seq <= 64) {
@@ -151,9 +124,9 @@ __device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, in
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
     // fewer than 2^31 items: each has a workgroup
-    auto count = [&](int chunk) -> int64_t { return wave_sum(tiles * max(1, (s.L + chunk - 1) / chunk)); };
-    const int chunk = choose_chunk(a, work, wave_sum(tiles), count);
-    const int n = tiles * a.c.Hkv * max(1, (s.L + chunk - 1) / chunk);
+    auto count = [&](int chunk) -> int64_t { return wave_sum(tiles * chunks_of(s.L, chunk)); };
+    const int chunk = choose_chunk(work, wave_sum(tiles), a.c.Hkv, a.target, count);
+    const int n = tiles * a.c.Hkv * chunks_of(s.L, chunk);
     int end = n;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -179,18 +152,18 @@ __device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, in
       int64_t n = 0, bef;
       for (int b = tid; b < a.n_seq; b += NT) {
         const Seq s = sequence(a, b);
-        n += (int64_t)tiles_of<ROWS>(a, s) * max(1, (s.L + chunk - 1) / chunk);
+        n += (int64_t)tiles_of<ROWS>(a, s) * chunks_of(s.L, chunk);
       }
       return block_scan<NT>(n, &bef, sh64);
     };
-    const int chunk = choose_chunk(a, work, tiles, count);
+    const int chunk = choose_chunk(work, tiles, a.c.Hkv, a.target, count);
     if (tid == 0) sh[0] = -1;
     int64_t base = 0;
     for (int b0 = 0; b0 < a.n_seq && base <= it; b0 += NT) {
       const int b = b0 + tid;
       Seq s = {0, 0, 0};
       if (b < a.n_seq) s = sequence(a, b);
-      const int64_t n = (int64_t)tiles_of<ROWS>(a, s) * a.c.Hkv * max(1, (s.L + chunk - 1) / chunk);
+      const int64_t n = (int64_t)tiles_of<ROWS>(a, s) * a.c.Hkv * chunks_of(s.L, chunk);
       const int64_t all = block_scan<NT>(n, &before, sh64);
       if (it >= base + before && it < base + before + n) {
         sh[0] = b;
