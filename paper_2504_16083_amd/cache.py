@@ -5,7 +5,7 @@ As in mmi.py the functions have the C names and marshal arguments only; what
 the C side cannot see (types, shapes and devices of the tensors) is checked
 here with ValueError, the rest by the library (MMIError). Tensors are torch
 device tensors on the context's device; their strides are passed on, the last
-dimension must be contiguous. Work goes to `stream`, or to the device's
+dimension must be contiguous, the others not broadcast. Work goes to `stream`, or to the device's
 current stream."""
 from __future__ import annotations
 
@@ -97,6 +97,8 @@ def _rows(ctx, name, t, n, heads):
                     sh = D
                 if rows <= 1:
                     ss = max(sh * h, D)
+                if ss <= 0 or sh <= 0:             # two zeros would be read as packed
+                    raise ValueError(f"{name} is broadcast over tokens or heads")
                 return ss, sh
             raise ValueError(f"the last dimension of {name} must be contiguous")
     if t.dtype != _BF16 or t.dim() != 3 or t.shape[2] != D:

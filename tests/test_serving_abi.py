@@ -223,3 +223,48 @@ def test_tree_binding_refusals():
     assert (t.row_start, t.length, t.pages, t.mask) == tuple(x.data_ptr() for x in (tree.row_start, tree.length, tree.pages, mask))
     assert [getattr(t, f"{x}_stride_{y}") for x in "qkvo" for y in "sh"] == list(range(8, 72, 8))
     assert t.scale == 0.5 and t.reserved == 0
+
+
+class _Host:
+    """A context whose tensors are the host's: the binding takes them, the library refuses the missing context."""
+    device, h = -1, None
+
+
+def _calls(n, q, k, v):
+    """Every entry point that takes rows, on tensors [n, heads, 128] given in each place in turn."""
+    new = lambda t: torch.zeros(*t.shape, dtype=torch.bfloat16)  # noqa: E731
+    cache = KV.Cache("bf16", *(torch.zeros(3, k.shape[1], 16, 128, dtype=torch.bfloat16) for _ in "kv"))
+    slot = torch.zeros(n, dtype=torch.int64)
+    tree = KV.Tree(torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32),
+                   torch.zeros(1, 3, dtype=torch.int32), max_rows=n)
+    ws = torch.zeros(16, dtype=torch.uint8)
+    return [lambda: KV.mmi_rope(_Host, KV.RopeCfg(), q=q, stream=0), lambda: KV.mmi_rope(_Host, KV.RopeCfg(), k=k, stream=0),
+            lambda: KV.mmi_rope(_Host, KV.RopeCfg(), q=new(q), q_out=q, stream=0),
+            lambda: KV.mmi_rope(_Host, KV.RopeCfg(), k=new(k), k_out=k, stream=0),
+            lambda: KV.mmi_cache_write(_Host, cache, k, new(v), slot, stream=0),
+            lambda: KV.mmi_cache_write(_Host, cache, new(k), v, slot, stream=0),
+            lambda: KV.mmi_cache_read(_Host, cache, slot, k, new(v), stream=0),
+            lambda: KV.mmi_cache_read(_Host, cache, slot, new(k), v, stream=0),
+            lambda: KV.mmi_tree_attention(_Host, cache, tree, q, new(k), new(v), new(q), ws, stream=0),
+            lambda: KV.mmi_tree_attention(_Host, cache, tree, new(q), k, new(v), new(q), ws, stream=0),
+            lambda: KV.mmi_tree_attention(_Host, cache, tree, new(q), new(k), v, new(q), ws, stream=0),
+            lambda: KV.mmi_tree_attention(_Host, cache, tree, new(q), new(k), new(v), q, ws, stream=0)]
+
+
+@pytest.mark.parametrize("n,Hq,Hkv", [(64, 8, 2), (1, 8, 2), (64, 1, 1)])
+def test_broadcast_rows_are_refused(n, Hq, Hkv):
+    """A row repeated over tokens and heads has the strides 0, 0, which the library takes for packed: 128 channels
+    would be read, or written, as n * heads rows of them."""
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    for call in _calls(n, bf(n, Hq, 128), bf(n, Hkv, 128), bf(n, Hkv, 128)):
+        with pytest.raises(mmi.MMIError, match="ctx"):       # all but the context is right
+            call()
+    every = [lambda H: bf(1, 1, 128).expand(n, H, 128)]
+    if n > 1:
+        every.append(lambda H: bf(1, H, 128).expand(n, H, 128))
+    if Hkv > 1:
+        every.append(lambda H: bf(n, 1, 128).expand(n, H, 128))
+    for wide in every:
+        for call in _calls(n, wide(Hq), wide(Hkv), wide(Hkv)):
+            with pytest.raises(ValueError, match="broadcast|strides"):
+                call()
