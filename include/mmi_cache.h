@@ -158,7 +158,9 @@ int mmi_tree_workspace(mmi_ctx* ctx, const mmi_cache* cache, const mmi_tree* tre
  * (8 bits); o rounded once; lse: device float [Hq][n_rows] natural-log sums, or NULL. A
  * row that sees no key gets o = 0 and lse = -inf. A drafted token that a row
  * does not see has no part in it, whatever its K and V hold (infinities and
- * NaN too). Query head h reads KV head h / (Hq / Hkv). o must not overlap an
+ * NaN too). In what a row sees an infinity or a NaN of V acts by the formula,
+ * but that weights under 2^-126 of the row's largest may be 0 (times an
+ * infinity: NaN). Query head h reads KV head h / (Hq / Hkv). o must not overlap an
  * input. workspace: 16-byte aligned device memory of at least
  * mmi_tree_workspace bytes; its contents do not matter before and after, but
  * calls (and replays of captured ones) that may run at the same time need one

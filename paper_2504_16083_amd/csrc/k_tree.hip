@@ -1088,6 +1088,13 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
     __builtin_amdgcn_sched_barrier(0);
     load(odd, min(3, steps - 1));
     advance();
+    // The slot before unit 0 has no V yet: its P is zero, and what it takes for
+    // V, the stage before stage 0, has to be finite (step 1 overwrites it).
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x4 none = {};
+      *reinterpret_cast<u32x4*>(&st[NST - 1].v[(tid / 16 + 32 * i) * TV + tid % 16 * 8]) = none;
+    }
     __syncthreads();
     // unit u: stage u / 2, block u % 2 (one key group), or stage u, block wk (two)
     const int units = WK == 1 ? 2 * steps : steps;
@@ -1103,12 +1110,10 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
     for (int x = 0; x < 2; ++x) p0[x] = p1[x] = zero8();
 #pragma unroll
     for (int x = 0; x < 8; ++x) s0 = mfma32(slot_operand(x, k_at(0), nullptr), r.q[x], s0);
-    // The slot before unit 0 has no V yet: its P is zero, and unit 0's own
-    // block stands in for it.
     constexpr bool PRE = WK == 1;
     if (PRE) {
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) op[i] = slot_operand(i, k_at(1), v_at(0));
+      for (int i = 0; i < AHEAD; ++i) op[i] = slot_operand(i, k_at(1), nullptr);
     }
     // Stage t + 2 into LDS, t + 4 on its way. Nothing here is left out at the
     // end (the last stage is loaded again, from the caches): where loads are
@@ -1134,7 +1139,7 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
     auto first_slot = [&](int u) INLINE {                         // u even: scores in s0
       if (!active) return;
       mask(s0, u);
-      slot<WL, PRE>(r, op, s0, s1, p1, p0, a.sc, k_at(u + 1), v_at(max(u - 1, 0)), k_at(u + 2), v_at(u));
+      slot<WL, PRE>(r, op, s0, s1, p1, p0, a.sc, k_at(u + 1), v_at(u - 1), k_at(u + 2), v_at(u));
     };
     auto second_slot = [&](int u) INLINE {
       if (!active) return;
