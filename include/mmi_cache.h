@@ -30,9 +30,11 @@ extern "C" {
  * a = position * f_i and is multiplied by attn_factor m:
  *   (x, y) -> (m (x cos a - y sin a), m (y cos a + x sin a)),
  * f_i = theta^(-2 i / rot_dim) radians a position, changed by `scaling`; the
- * other channels stay as they are. Angles are exact to 2^-25 of a turn at any
- * 32-bit position (64-bit fixed point), the products are taken in fp32 and
- * rounded to bfloat16 once. */
+ * other channels stay as they are. The angle of a position and of f_i as a
+ * double (what mmi_rope_freq returns, or inv_freq) is held to 2^-25 of a turn
+ * at any 32-bit position (64-bit fixed point); mmi_rope_freq's double is off
+ * from the formula by up to (ln theta + 8) 2^-53 of itself, which a position p
+ * multiplies. The products are taken in fp32 and rounded to bfloat16 once. */
 #define MMI_ROPE_HALF 0          /* pair i = channels i and i + rot_dim / 2 */
 #define MMI_ROPE_INTERLEAVED 1   /* pair i = channels 2 i and 2 i + 1 */
 
@@ -57,11 +59,12 @@ typedef struct mmi_rope_cfg {
   double orig_len;               /* PARTS: > 0 */
   double beta_fast, beta_slow;   /* PARTS: beta_fast > beta_slow >= 0 */
   double attn_factor;            /* m > 0; 0: 0.1 ln(factor) + 1 for PARTS, else 1 */
-  const double* inv_freq;        /* HOST array [rot_dim / 2] of f_i, finite and >= 0, in place of theta
+  const double* inv_freq;        /* HOST array [rot_dim / 2] of f_i in [0, 2^40], in place of theta
                                     and scaling (factor still sets m of PARTS), or NULL */
 } mmi_rope_cfg;
 
-/* The frequencies f_i of a configuration: HOST array [rot_dim / 2]. Computing
+/* The frequencies f_i of a configuration (up to 2^40, else
+ * MMI_ERR_BAD_CONFIG): HOST array [rot_dim / 2]. Computing
  * them takes longer than a short call's other host work; a program that calls
  * mmi_rope for single tokens keeps them in inv_freq. */
 int mmi_rope_freq(const mmi_rope_cfg* cfg, double* inv_freq);

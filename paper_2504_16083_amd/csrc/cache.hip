@@ -36,6 +36,8 @@ void strides(int64_t& ss, int64_t& sh, int H, const char* name) {
 }
 
 constexpr double TWO_PI = 6.283185307179586476925286766559;
+constexpr double PER_TURN = 0x1.45f306dc9c883p-3, PER_TURN_REST = -0x1.6b01ec5417056p-57;   // 1 / (2 pi) as the sum of two
+constexpr double MOST_FREQ = 0x1p40;
 constexpr int ROW_BYTES[4] = {256, 128, 128, 64};
 
 }  // namespace
@@ -72,7 +74,7 @@ double rope_freq(const mmi_rope_cfg* cfg, double* freq) {
         f *= g + (1.0 - g) / c.factor;
       }
     }
-    if (!(f >= 0 && std::isfinite(f))) fail(MMI_ERR_BAD_CONFIG, "frequency %d is not a finite positive number", i);
+    if (!(f >= 0 && f <= MOST_FREQ)) fail(MMI_ERR_BAD_CONFIG, "frequency %d is not in [0, 2^40]", i);
     freq[i] = f;
   }
   return c.attn_factor > 0 ? c.attn_factor : c.scaling == MMI_ROPE_SCALE_PARTS ? 0.1 * std::log(c.factor) + 1.0 : 1.0;
@@ -114,8 +116,12 @@ RopeArgs rope_args(const mmi_problem& p, const mmi_rope_cfg* cfg, const int32_t*
   a.sec2 = sum ? c.sections[0] + c.sections[1] : half;
   a.m = (float)m;
   for (int i = 0; i < half; ++i) {
-    const double t = freq[i] * (1.0 / TWO_PI), part = t - std::floor(t);
-    a.turn[i] = (uint64_t)(part * 18446744073709551616.0);   // below 2^64: the fraction is at most 1 - 2^-53
+    // turns to 2^-63: a product of doubles alone would be off by up to 2^-53
+    // of itself, which a far position multiplies. f <= 2^40, so the second
+    // part stays below 2^50 in units of 2^-64.
+    const double t = freq[i] * PER_TURN, rest = std::fma(freq[i], PER_TURN, -t) + freq[i] * PER_TURN_REST;
+    const double part = t - std::floor(t);                   // exact, at most 1 - 2^-53
+    a.turn[i] = (uint64_t)(part * 0x1p64) + (uint64_t)std::llrint(rest * 0x1p64);
   }
   return a;
 }

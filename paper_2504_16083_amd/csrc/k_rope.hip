@@ -10,9 +10,10 @@
 // what is still to be read: 64 us for 67 at 20240 tokens, the same at 262144.
 //
 // Angles: turns a position as a 64-bit fraction, times the position, modulo
-// 2^64: the fraction of a turn that is left, exact at any position (in fp32 a
-// position of 2^20 and more has lost the angle's fraction). Its upper 32 bits
-// as a signed number are the angle in [-1/2, 1/2) turns.
+// 2^64: the fraction of a turn that is left, to 2^-32 at position 2^31 (in
+// fp32 a position of 2^20 and more has lost the angle's fraction). Its upper
+// 32 bits as a signed number are the angle in [-1/2, 1/2) turns; as fp32 that
+// is off by up to 2^-26.
 #include <algorithm>
 
 #include "cache.hpp"

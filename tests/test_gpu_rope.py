@@ -154,3 +154,36 @@ def test_stream_and_graph(ctx):
         KV.mmi_rope(ctx, cfg, q, k, q_out=want_q, k_out=want_k)
         torch.cuda.synchronize()
         assert torch.equal(a, want_q) and torch.equal(b, want_k)
+
+
+def exact_turns(pos, f):
+    """position * f / (2 pi) modulo one, of whole numbers and doubles, by whole-number arithmetic."""
+    from fractions import Fraction
+    pi = Fraction(31415926535897932384626433832795028841971693993751058209749445923078164062862, 10 ** 76)
+    out = np.zeros((len(pos), len(f)))
+    for j, y in enumerate(f):
+        step = Fraction(float(y)) / (2 * pi)
+        for i, p in enumerate(pos):
+            t = int(p) * step
+            out[i, j] = float(t - round(t))
+    return out
+
+
+@pytest.mark.parametrize("top", [1.0, 100.0, 1e5, 2.0 ** 40])
+def test_angles_of_far_positions_and_high_frequencies(ctx, top):
+    """A caller's frequencies up to `top` radians a position, at positions up to the ends of 32 bits: the number of
+    turns is held to 2^-63 a position, 2^-32 at 2^31, and the fraction that is left rounded to fp32, half a step of
+    a number below 1/2: 2^-26 of a turn and less, inside what check() allows."""
+    from paper_2504_16083_amd import cache as KV
+    rng = np.random.default_rng(int(top))
+    f = np.sort(np.exp(rng.uniform(np.log(1e-7), np.log(top), 64)))[::-1].copy()
+    f[0] = top
+    pos = np.concatenate([[0, 1, -1, 2 ** 31 - 1, -(2 ** 31)], rng.integers(-(2 ** 31), 2 ** 31, 120),
+                          rng.integers(0, 1 << 21, 120)])
+    q = rand((len(pos), 2, D), 31)
+    out = torch.empty_like(q)
+    KV.mmi_rope(ctx, KV.RopeCfg(inv_freq=f), q=q, q_out=out, pos=torch.tensor(pos, dtype=torch.int32).cuda())
+    x, angle = f64(q), 2 * np.pi * exact_turns(pos, f)[:, None]
+    a, b = x[..., :64], x[..., 64:]
+    want = np.concatenate([a * np.cos(angle) - b * np.sin(angle), b * np.cos(angle) + a * np.sin(angle)], -1)
+    check(out, q, want, 1.0, f, "half")

@@ -268,3 +268,34 @@ def test_broadcast_rows_are_refused(n, Hq, Hkv):
         for call in _calls(n, wide(Hq), wide(Hkv), wide(Hkv)):
             with pytest.raises(ValueError, match="broadcast|strides"):
                 call()
+
+
+@pytest.mark.parametrize("theta", [100.0, 1e4, 1e6, 3e7])
+@pytest.mark.parametrize("scaling,factor", [("none", 1.0), ("linear", 3.0), ("ntk", 8.0), ("parts", 40.0)])
+def test_rope_frequencies_to_the_last_places(theta, scaling, factor):
+    """mmi_rope_freq against the formula in 50 digits: off by (ln theta + 8) 2^-53 of itself at most."""
+    from decimal import Decimal, getcontext
+    getcontext().prec = 50
+    pi = Decimal("3.1415926535897932384626433832795028841971693993751")
+    for rot in (16, 48, 96, 128):
+        cfg = KV.RopeCfg(rot_dim=rot, theta=theta, scaling=scaling, factor=factor, orig_len=32768.0)
+        base, F = Decimal(theta), Decimal(factor)
+        if scaling == "ntk":
+            base = base * F ** (Decimal(rot) / (rot - 2))
+        for i in range(rot // 2):
+            f = base ** (Decimal(-2 * i) / rot)
+            if scaling == "linear":
+                f /= F
+            if scaling == "parts":
+                g = min(max((32768 * f / (2 * pi) - 1) / 31, Decimal(0)), Decimal(1))
+                f *= g + (1 - g) / F
+            off = abs(Decimal(cfg.c[0].inv_freq[i]) / f - 1)
+            assert off <= (base.ln() + 8) * Decimal(2) ** -53, (rot, i, off)
+
+
+def test_rope_frequencies_end_at_2_to_40():
+    table = (ct.c_double * 64)(*[2.0 ** 40] * 64)
+    assert rope(inv_freq=table) == INVALID and "ctx" in mmi.mmi_last_error()
+    table[5] = 2.0 ** 40 * (1 + 2.0 ** -52)
+    assert rope(inv_freq=table) == BAD_CONFIG
+    assert rope(theta=1e-20) == BAD_CONFIG and rope(theta=1e-12) == INVALID
