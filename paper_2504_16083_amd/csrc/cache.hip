@@ -80,8 +80,20 @@ double rope_freq(const mmi_rope_cfg* cfg, double* freq) {
   return c.attn_factor > 0 ? c.attn_factor : c.scaling == MMI_ROPE_SCALE_PARTS ? 0.1 * std::log(c.factor) + 1.0 : 1.0;
 }
 
-RopeArgs rope_args(const mmi_problem& p, const mmi_rope_cfg* cfg, const int32_t* pos, const void* q, const void* k,
+// Of the problem only what the rotation uses: the limits that the attention
+// kernel sets to K's strides are not its own.
+RopeArgs rope_args(const mmi_problem* prob, const mmi_rope_cfg* cfg, const int32_t* pos, const void* q, const void* k,
                    void* q_out, void* k_out) {
+  if (!prob) fail(MMI_ERR_INVALID_ARG, "problem is NULL");
+  mmi_problem p = *prob;
+  if (p.S < 1) fail(MMI_ERR_INVALID_ARG, "S must be >= 1");
+  if (p.S > MMI_MAX_SEQ) fail(MMI_ERR_UNSUPPORTED, "S = %lld exceeds %d", (long long)p.S, MMI_MAX_SEQ);
+  if (p.Hq < 1 || p.Hkv < 1) fail(MMI_ERR_INVALID_ARG, "head counts must be >= 1");
+  if (p.Hq % p.Hkv) fail(MMI_ERR_UNSUPPORTED, "Hq %% Hkv != 0");
+  if (p.D != D) fail(MMI_ERR_UNSUPPORTED, "head dim %d (only 128)", p.D);
+  if (p.block != MMI_BLOCK) fail(MMI_ERR_UNSUPPORTED, "block %d (only 64)", p.block);
+  strides(p.q_stride_s, p.q_stride_h, p.Hq, "q");
+  strides(p.k_stride_s, p.k_stride_h, p.Hkv, "k");
   double freq[D / 2];
   const double m = rope_freq(cfg, freq);
   const mmi_rope_cfg& c = *cfg;

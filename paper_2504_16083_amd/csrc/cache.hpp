@@ -106,7 +106,7 @@ __host__ __device__ inline int choose_chunk(int64_t work, int64_t tiles, int Hkv
 // ---------------------------------------------------------------- cache.hip
 // Host checks (they throw Error) and the records for the launches.
 double rope_freq(const mmi_rope_cfg* cfg, double* freq);
-RopeArgs rope_args(const mmi_problem& p, const mmi_rope_cfg* cfg, const int32_t* pos, const void* q, const void* k,
+RopeArgs rope_args(const mmi_problem* prob, const mmi_rope_cfg* cfg, const int32_t* pos, const void* q, const void* k,
                    void* q_out, void* k_out);
 CacheDev cache_dev(const mmi_cache* c);
 RowsArgs rows_args(const mmi_cache* c, const void* k, int64_t k_ss, int64_t k_sh, const void* v, int64_t v_ss,

@@ -1629,11 +1629,7 @@ int mmi_rope_freq(const mmi_rope_cfg* cfg, double* inv_freq) {
 int mmi_rope(mmi_ctx* ctx, const mmi_problem* prob, const mmi_rope_cfg* cfg, const int32_t* pos, const void* q,
              const void* k, void* q_out, void* k_out, void* stream) {
   return guarded([&] {
-    if (!prob) fail(MMI_ERR_INVALID_ARG, "problem is NULL");
-    mmi_problem p = *prob;
-    p.modality = nullptr;          // not read here, nor are the strides of v and o
-    p.v_stride_s = p.v_stride_h = p.o_stride_s = p.o_stride_h = 0;
-    const RopeArgs a = rope_args(normalise(&p), cfg, pos, q, k, q_out, k_out);
+    const RopeArgs a = rope_args(prob, cfg, pos, q, k, q_out, k_out);
     if (!ctx) fail(MMI_ERR_INVALID_ARG, "ctx is NULL");
     OnDevice d(ctx->device);
     HIPCHK(launch_rope(a, cfg->layout, (hipStream_t)stream));

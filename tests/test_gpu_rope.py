@@ -187,3 +187,18 @@ def test_angles_of_far_positions_and_high_frequencies(ctx, top):
     a, b = x[..., :64], x[..., 64:]
     want = np.concatenate([a * np.cos(angle) - b * np.sin(angle), b * np.cos(angle) + a * np.sin(angle)], -1)
     check(out, q, want, 1.0, f, "half")
+
+
+def test_long_prompt_in_a_fused_projection(ctx):
+    """Q and K of 524289 tokens as views of one projection, rotated in place: K's token stride times the length
+    passes 2^31 elements. As the same rows in tensors of their own."""
+    from paper_2504_16083_amd import cache as KV
+    S, Hq, Hkv = (1 << 19) + 1, 28, 4
+    fused = torch.empty(S, Hq + 2 * Hkv, D, dtype=torch.bfloat16, device="cuda")
+    fused.random_(-8, 8, generator=torch.Generator(device="cuda").manual_seed(1))
+    q, k = fused[:, :Hq], fused[:, Hq:Hq + Hkv]
+    qc, kc, v = q.contiguous(), k.contiguous(), fused[:, Hq + Hkv:].clone()
+    cfg = KV.RopeCfg(theta=1e6)
+    KV.mmi_rope(ctx, cfg, qc, kc)
+    KV.mmi_rope(ctx, cfg, q, k)
+    assert torch.equal(q, qc) and torch.equal(k, kc) and torch.equal(fused[:, Hq + Hkv:], v)

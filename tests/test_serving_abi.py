@@ -299,3 +299,14 @@ def test_rope_frequencies_end_at_2_to_40():
     table[5] = 2.0 ** 40 * (1 + 2.0 ** -52)
     assert rope(inv_freq=table) == BAD_CONFIG
     assert rope(theta=1e-20) == BAD_CONFIG and rope(theta=1e-12) == INVALID
+
+
+@pytest.mark.parametrize("S", [524288, 1048576, 1 << 21])
+def test_rope_takes_long_fused_projections(S):
+    """Views of a [S, 36, 128] projection: K's token stride times S passes 2^31 elements, a limit of the attention
+    kernel's and not of the rotation."""
+    wide = {"q": (36 * 128, 128), "k": (36 * 128, 128)}
+    assert rope(mmi.Problem(S, 28, 4, strides=wide)) == INVALID and "ctx" in mmi.mmi_last_error()
+    assert rope(mmi.Problem(S, 28, 4, strides={"k": (1 << 30, 1 << 24)})) == INVALID and "ctx" in mmi.mmi_last_error()
+    assert rope(mmi.Problem(S, 28, 4, strides={"k": (1 << 41, 128)})) == UNSUPPORTED
+    assert rope(mmi.Problem((1 << 21) + 1, 28, 4)) == UNSUPPORTED
