@@ -119,6 +119,21 @@ def _array(ctx, name, t, dtype, shape):
     return t.data_ptr()
 
 
+def _kept(i, what):
+    """Property: tensor i of what the object was made of, of which it has handed the address on."""
+    def same(self, t):                             # x.t += 1 ends here with the tensor itself
+        if t is not self._tensors[i]:
+            raise AttributeError(f"a {what} keeps its tensors; make another one for others")
+    return property(lambda self: self._tensors[i], same)
+
+
+_data_ptr = torch.Tensor.data_ptr
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
 # ------------------------------------------------------------------ rotary positions
 class RopeCfg:
     """Rotation of the first rot_dim channels (mmi_rope_cfg). layout: "half"
@@ -189,15 +204,17 @@ class Cache:
     """The memory of a paged cache (mmi_cache). k, v: [n_pages, Hkv, page, 128]
     bfloat16 for type "bf16", else uint8 [n_pages, Hkv, page, bytes a row]
     (128 for "fp8" and "int8", 64 for "fp4") with k_scale, v_scale uint8
-    [n_pages, Hkv, page, 4]; only the first dimension may be strided."""
+    [n_pages, Hkv, page, 4]; only the first dimension may be strided. The
+    tensors stay the cache's, with the memory that they had when it was made."""
 
     def __init__(self, type, k, v, k_scale=None, v_scale=None):
         if type not in TYPES:
             raise ValueError(f"cache type {type!r} is unknown")
-        self.type, self.k, self.v, self.k_scale, self.v_scale = type, k, v, k_scale, v_scale
+        bf16 = type == "bf16"
+        self.type = type
+        self._tensors = (k, v, None, None) if bf16 else (k, v, k_scale, v_scale)
         self.n_pages, self.Hkv, self.page = k.shape[:3]
         want = (self.n_pages, self.Hkv, self.page)
-        bf16 = type == "bf16"
         self.device, self.index = k.device, k.get_device()
         row = D if bf16 else ROW_BYTES[type]
         stride = self._pool("k", k, torch.bfloat16 if bf16 else torch.uint8, want + (row,))
@@ -210,12 +227,13 @@ class Cache:
             scale = self._pool("k_scale", k_scale, torch.uint8, want + (4,))
             if self._pool("v_scale", v_scale, torch.uint8, want + (4,)) != scale:
                 raise ValueError("k_scale and v_scale must have the same strides")
-        else:
-            self.k_scale = self.v_scale = None
-        self.c = mmi_cache(TYPES[type], self.page, self.Hkv, D, self.n_pages, k.data_ptr(), v.data_ptr(),
-                           None if bf16 else k_scale.data_ptr(), None if bf16 else v_scale.data_ptr(),
+        self.c = mmi_cache(TYPES[type], self.page, self.Hkv, D, self.n_pages, *map(_ptr, self._tensors),
                            stride * (2 if bf16 else 1), scale)
+        self._used = [t for t in self._tensors if t is not None]
+        self._at = [*map(_data_ptr, self._used)]
         self.ref = ct.byref(self.c)
+
+    k, v, k_scale, v_scale = (_kept(i, "cache") for i in range(4))
 
     def _pool(self, name, t, dtype, shape):
         if t.dtype != dtype or tuple(t.shape) != shape:
@@ -245,6 +263,8 @@ class Cache:
 def _on(ctx, cache):
     if cache.index != ctx.device:
         raise ValueError(f"the cache is on {cache.device}, the context on device {ctx.device}")
+    if [*map(_data_ptr, cache._used)] != cache._at:
+        raise ValueError("the cache's tensors have been given other memory")
 
 
 def mmi_cache_write(ctx, cache, k, v, slot, stream=None):
@@ -273,7 +293,7 @@ class Tree:
     max_pages], mask int64 [n_rows, words] (bit j of a row: it sees drafted
     token j; None: token i sees 0 .. i), max_rows and max_len the most drafted
     and cached tokens of a sequence. The tensors are checked once, here, and
-    stay the batch's; their contents may change between calls, within these
+    stay the batch's, with the memory that they have; their contents may change between calls, within these
     bounds, and so may max_rows, max_len and scale."""
 
     def __init__(self, row_start, length, pages, mask=None, max_rows=1, max_len=0, scale=0.0):
@@ -284,30 +304,28 @@ class Tree:
             raise ValueError("pages must be a tensor [n_seq, max_pages], mask one [n_rows, words]")
         self._max_pages = pages.shape[1]
         self._mask_rows, self._words = (None, 0) if mask is None else mask.shape
-        self._ptr = (self._array("row_start", row_start, torch.int32, (self._n_seq + 1,)),
-                     self._array("length", length, torch.int32, (self._n_seq,)),
-                     self._array("pages", pages, torch.int32, (self._n_seq, self._max_pages)),
-                     None if mask is None else self._array("mask", mask, torch.int64, tuple(mask.shape)))
+        self._check("row_start", row_start, torch.int32, (self._n_seq + 1,))
+        self._check("length", length, torch.int32, (self._n_seq,))
+        self._check("pages", pages, torch.int32, (self._n_seq, self._max_pages))
+        if mask is not None:
+            self._check("mask", mask, torch.int64, tuple(mask.shape))
+        self._ptr = tuple(map(_ptr, self._tensors))
+        self._used = [t for t in self._tensors if t is not None]
+        self._at = [*map(_data_ptr, self._used)]
 
-    def _held(i):
-        def same(self, t):                         # tree.length += 1 ends here with the tensor itself
-            if t is not self._tensors[i]:
-                raise AttributeError("a batch keeps its tensors; make another Tree for others")
-        return property(lambda self: self._tensors[i], same)
+    row_start, length, pages, mask = (_kept(i, "batch") for i in range(4))
 
-    row_start, length, pages, mask = _held(0), _held(1), _held(2), _held(3)
-    del _held
-
-    def _array(self, name, t, dtype, shape):
+    def _check(self, name, t, dtype, shape):
         if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape}")
         if t.get_device() != self.index:
             raise ValueError(f"{name} is on {t.device}, length on {self.length.device}")
-        return t.data_ptr()
 
     def _struct(self, ctx, Hq, n_rows, *strides):
         if self.index != ctx.device:
             raise ValueError(f"the tree is on {self.length.device}, the context on device {ctx.device}")
+        if [*map(_data_ptr, self._used)] != self._at:
+            raise ValueError("the batch's tensors have been given other memory")
         if self._mask_rows is not None and self._mask_rows != n_rows:
             raise ValueError(f"mask has {self._mask_rows} rows for {n_rows} of q")
         if not strides:

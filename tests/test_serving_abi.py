@@ -310,3 +310,43 @@ def test_rope_takes_long_fused_projections(S):
     assert rope(mmi.Problem(S, 28, 4, strides={"k": (1 << 30, 1 << 24)})) == INVALID and "ctx" in mmi.mmi_last_error()
     assert rope(mmi.Problem(S, 28, 4, strides={"k": (1 << 41, 128)})) == UNSUPPORTED
     assert rope(mmi.Problem((1 << 21) + 1, 28, 4)) == UNSUPPORTED
+
+
+def _moved(how, t):
+    """t with its memory replaced by a longer tensor's."""
+    other = torch.zeros(4, *t.shape, dtype=t.dtype)
+    if how == "set":
+        t.set_(other[1])
+    elif how == "data":
+        t.data = other[1]
+    else:
+        t.resize_(64 * t.numel() + 4096)
+        assert t.numel() > 4096
+
+
+@pytest.mark.parametrize("how", ["set", "data", "resize"])
+@pytest.mark.parametrize("which", ["k", "v", "k_scale", "v_scale", "row_start", "length", "pages", "mask"])
+def test_tensors_with_other_memory_are_refused(how, which):
+    """A cache and a batch hand addresses on that they took when they were made: a tensor that has been given other
+    memory since must not be read or written at the old one. Another tensor in its place is no assignment."""
+    cache = KV.Cache("fp8", *(torch.zeros(3, 2, 16, w, dtype=torch.uint8) for w in (128, 128, 4, 4)))
+    tree = KV.Tree(torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32),
+                   torch.zeros(1, 3, dtype=torch.int32), mask=torch.zeros(5, 1, dtype=torch.int64), max_rows=5)
+    bf = lambda h: torch.zeros(5, h, 128, dtype=torch.bfloat16)  # noqa: E731
+    slot, ws = torch.zeros(5, dtype=torch.int64), torch.zeros(16, dtype=torch.uint8)
+    calls = [lambda: KV.mmi_tree_attention(_Host, cache, tree, bf(4), bf(2), bf(2), bf(4), ws, stream=0)]
+    if which in ("k", "v", "k_scale", "v_scale"):
+        calls += [lambda: KV.mmi_cache_write(_Host, cache, bf(2), bf(2), slot, stream=0),
+                  lambda: KV.mmi_cache_read(_Host, cache, slot, bf(2), bf(2), stream=0)]
+    owner = tree if len(calls) == 1 else cache
+    t = getattr(owner, which)
+    t += 1                                                   # the contents are the caller's
+    for call in calls:
+        with pytest.raises(mmi.MMIError, match="ctx"):
+            call()
+    with pytest.raises(AttributeError):
+        setattr(owner, which, t.clone())
+    _moved(how, t)
+    for call in calls:
+        with pytest.raises(ValueError, match="other memory"):
+            call()
