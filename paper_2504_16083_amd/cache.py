@@ -300,8 +300,9 @@ class Tree:
         self.max_rows, self.max_len, self.scale = max_rows, max_len, scale
         self._tensors = row_start, length, pages, mask
         self._n_seq, self.index = length.shape[0], length.get_device()
-        if pages.dim() != 2 or mask is not None and mask.dim() != 2:
-            raise ValueError("pages must be a tensor [n_seq, max_pages], mask one [n_rows, words]")
+        # a mask of no words has no address and would be taken for none
+        if pages.dim() != 2 or mask is not None and (mask.dim() != 2 or mask.shape[1] < 1):
+            raise ValueError("pages must be a tensor [n_seq, max_pages], mask one [n_rows, words], words >= 1")
         self._max_pages = pages.shape[1]
         self._mask_rows, self._words = (None, 0) if mask is None else mask.shape
         self._check("row_start", row_start, torch.int32, (self._n_seq + 1,))

@@ -350,3 +350,10 @@ def test_tensors_with_other_memory_are_refused(how, which):
     for call in calls:
         with pytest.raises(ValueError, match="other memory"):
             call()
+
+
+def test_mask_without_words_is_refused():
+    """Such a tensor has no address: the call would go on without a mask, every token seeing those before it."""
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError, match="words"):
+        KV.Tree(i32(2), i32(1), i32(1, 3), mask=torch.zeros(5, 0, dtype=torch.int64), max_rows=5)
