@@ -146,7 +146,7 @@ typedef struct mmi_tree {
   int64_t k_stride_s, k_stride_h;
   int64_t v_stride_s, v_stride_h;
   int64_t o_stride_s, o_stride_h;
-  float scale;                   /* of the scores, > 0; 0: 1 / sqrt(128) */
+  float scale;                   /* of the scores, > 0 (and below 2^127); 0: 1 / sqrt(128) */
   int32_t reserved;              /* 0 */
 } mmi_tree;
 

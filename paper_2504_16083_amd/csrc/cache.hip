@@ -8,6 +8,7 @@
 #include <cstdio>
 
 #include "cache.hpp"
+#include "device.hpp"
 
 namespace mmi {
 
@@ -210,7 +211,7 @@ mmi_tree tree_checked(const mmi_cache* c, const mmi_tree* tree) {
     fail(MMI_ERR_INVALID_ARG, "max_pages pages of %d tokens do not hold max_len", c->page);
   if (t.mask && t.mask_words < (t.max_rows + 63) / 64)
     fail(MMI_ERR_INVALID_ARG, "%d words of mask for %d drafted tokens", t.mask_words, t.max_rows);
-  if (!(t.scale >= 0 && std::isfinite(t.scale))) fail(MMI_ERR_INVALID_ARG, "scale must be positive, or 0");
+  if (!(t.scale >= 0 && std::isfinite(t.scale * LOG2E))) fail(MMI_ERR_INVALID_ARG, "scale must be positive, or 0");
   if (t.reserved) fail(MMI_ERR_INVALID_ARG, "reserved must be 0");
   strides(t.q_stride_s, t.q_stride_h, t.Hq, "q");
   strides(t.k_stride_s, t.k_stride_h, c->Hkv, "k");
@@ -241,7 +242,7 @@ TreeArgs tree_args(const mmi_cache* c, const mmi_tree& t, const void* q, const v
   a.mask = (const uint32_t*)t.mask;
   a.n_seq = t.n_seq; a.n_rows = t.n_rows; a.g = t.Hq / c->Hkv;
   a.max_rows = t.max_rows; a.max_len = (int32_t)t.max_len; a.max_pages = t.max_pages; a.mask_words = t.mask_words;
-  a.sc = (t.scale > 0 ? t.scale : 0.08838834764831845f) * 1.4426950408889634f;
+  a.sc = (t.scale > 0 ? t.scale : 0.08838834764831845f) * LOG2E;   // finite, above zero
   return a;
 }
 

@@ -357,3 +357,10 @@ def test_mask_without_words_is_refused():
     i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
     with pytest.raises(ValueError, match="words"):
         KV.Tree(i32(2), i32(1), i32(1, 3), mask=torch.zeros(5, 0, dtype=torch.int64), max_rows=5)
+
+
+def test_scale_that_overflows_is_refused():
+    """Scores are taken times scale * log2(e): an infinity there makes a score of zero a NaN."""
+    assert tree(scale=3e38) == (INVALID, INVALID) and "scale" in mmi.mmi_last_error()
+    for scale in (2.0 ** 127, 1.0, 1e-45):
+        assert tree(scale=scale) == (INVALID, INVALID) and "ctx" in mmi.mmi_last_error()
