@@ -54,15 +54,16 @@ struct TreeArgs {
   int32_t n_seq, n_rows, g, max_rows, max_len, max_pages, mask_words;
   float sc;                        // scale of the scores times log2(e)
   int32_t target;                  // workgroups that a batch is cut into, if it is long enough
-  int32_t items;                   // launched workgroups = partials the workspace holds
+  int32_t items;                   // launched workgroups
+  int32_t parts;                   // partials that the workspace holds
   int32_t cus;                     // compute units
-  float* part_o;                   // [items][rows of a tile][128], sums over P as it entered the product
-  float* part_ml;                  // [items][rows of a tile][4]: maximum (log2 units), sum of that P, fp32-P sum
-  int32_t* rec;                    // [n_seq][2]: a sequence's first item and the chunks of its keys
+  float* part_o;                   // [parts][rows of a tile][128], sums over P as it entered the product
+  float* part_ml;                  // [parts][rows of a tile][4]: maximum (log2 units), sum of that P, fp32-P sum
+  int32_t* rec;                    // [n_seq][2]: place of a sequence's first partial, and the chunks of its keys
 };
 struct TreeShape {                 // how a batch is cut, from its bounds alone
   int32_t rows;                    // query rows of a workgroup's tile
-  int32_t target, items;
+  int32_t target, items, parts;
   size_t part_o, part_ml, rec, bytes;   // offsets into the workspace, and its size
 };
 TreeShape tree_shape(const mmi_tree& t, int Hkv, int type, int cus);

@@ -75,6 +75,7 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* before, int64_
 
 struct Item {
   int b, first, chunks, chunk, tile, head;   // sequence, its first item, its chunks; this one's chunk, tile, head
+  int part;                                  // place of its partial, if the sequence is cut
   int c0, c1;                                // cached tokens
   Seq seq;
 };
@@ -82,11 +83,13 @@ struct Item {
 template <int ROWS>
 __device__ __forceinline__ int tiles_of(const TreeArgs& a, const Seq& s) { return (s.T * a.g + ROWS - 1) / ROWS; }
 
-__device__ __forceinline__ void set_item(const TreeArgs& a, Item& r, int it, int b, int first, int tiles, int chunk,
-                                         const Seq& s) {
+// first, part: items of the sequences before it, and those of them that are cut.
+__device__ __forceinline__ void set_item(const TreeArgs& a, Item& r, int it, int b, int first, int part, int tiles,
+                                         int chunk, const Seq& s) {
   const int at = it - first;
   r.b = b;
   r.first = first;
+  r.part = part + at;
   r.seq = s;
   r.chunks = chunks_of(s.L, chunk);
   r.chunk = at / (tiles * a.c.Hkv);
@@ -114,7 +117,7 @@ __device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, in
     auto count = [&](int chunk) -> int64_t { return (int64_t)tiles * chunks_of(s.L, chunk); };
     const int chunk = choose_chunk((int64_t)tiles * s.L, tiles, a.c.Hkv, a.target, count);
     if (it >= count(chunk) * a.c.Hkv) return false;
-    set_item(a, r, it, 0, 0, tiles, chunk, s);
+    set_item(a, r, it, 0, 0, 0, tiles, chunk, s);
   } else if (a.n_seq <= 64) {
     const int lane = tid & 63;
     Seq s = {0, 0, 0};
@@ -126,19 +129,22 @@ __device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, in
     // fewer than 2^31 items: each has a workgroup
     auto count = [&](int chunk) -> int64_t { return wave_sum(tiles * chunks_of(s.L, chunk)); };
     const int chunk = choose_chunk(work, wave_sum(tiles), a.c.Hkv, a.target, count);
-    const int n = tiles * a.c.Hkv * chunks_of(s.L, chunk);
-    int end = n;
+    const int n = tiles * a.c.Hkv * chunks_of(s.L, chunk), cut = s.L > chunk ? n : 0;
+    int end = n, parts = cut;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-      const int y = __shfl_up(end, d);
-      if (lane >= d) end += y;
+      const int y = __shfl_up(end, d), z = __shfl_up(parts, d);
+      if (lane >= d) {
+        end += y;
+        parts += z;
+      }
     }
     const uint64_t mine = __ballot(it >= end - n && it < end);
     if (!mine) return false;
     const int b = __builtin_ctzll(mine);
     auto of = [&](int x) { return __builtin_amdgcn_readlane(x, b); };
     const Seq sb = {of(s.row0), of(s.T), of(s.L)};
-    set_item(a, r, it, b, of(end - n), of(tiles), chunk, sb);
+    set_item(a, r, it, b, of(end - n), of(parts - cut), of(tiles), chunk, sb);
   } else {
     int64_t work = 0, tiles = 0, before;
     for (int b = tid; b < a.n_seq; b += NT) {
@@ -158,33 +164,36 @@ __device__ __forceinline__ bool find_item(const TreeArgs& a, int it, Item& r, in
     };
     const int chunk = choose_chunk(work, tiles, a.c.Hkv, a.target, count);
     if (tid == 0) sh[0] = -1;
-    int64_t base = 0;
-    for (int b0 = 0; b0 < a.n_seq && base <= it; b0 += NT) {
+    uint64_t base = 0;                     // items in the lower half, those of cut sequences in the upper one
+    for (int b0 = 0; b0 < a.n_seq && (uint32_t)base <= (uint32_t)it; b0 += NT) {
       const int b = b0 + tid;
       Seq s = {0, 0, 0};
       if (b < a.n_seq) s = sequence(a, b);
-      const int64_t n = (int64_t)tiles_of<ROWS>(a, s) * a.c.Hkv * chunks_of(s.L, chunk);
-      const int64_t all = block_scan<NT>(n, &before, sh64);
-      if (it >= base + before && it < base + before + n) {
+      const uint32_t n = tiles_of<ROWS>(a, s) * a.c.Hkv * chunks_of(s.L, chunk);
+      const int64_t all = block_scan<NT>((int64_t)(s.L > chunk ? (uint64_t)n << 32 | n : n), &before, sh64);
+      const uint64_t at = base + (uint64_t)before;
+      if ((uint32_t)it >= (uint32_t)at && (uint32_t)it < (uint32_t)at + n) {
         sh[0] = b;
-        sh[1] = (int)(base + before);
+        sh[1] = (int)(uint32_t)at;
+        sh[2] = (int)(at >> 32);
       }
-      base += all;
+      base += (uint64_t)all;
     }
     __syncthreads();
     const int b = __builtin_amdgcn_readfirstlane(sh[0]);
     if (b < 0) return false;
     const Seq s = sequence(a, b);
-    set_item(a, r, it, b, __builtin_amdgcn_readfirstlane(sh[1]), tiles_of<ROWS>(a, s), chunk, s);
+    set_item(a, r, it, b, __builtin_amdgcn_readfirstlane(sh[1]), __builtin_amdgcn_readfirstlane(sh[2]),
+             tiles_of<ROWS>(a, s), chunk, s);
   }
   // the same in every lane: into scalar registers, or every branch on them is a divergent one
-  for (int* x : {&r.b, &r.first, &r.chunks, &r.chunk, &r.tile, &r.head, &r.c0, &r.c1, &r.seq.row0, &r.seq.T, &r.seq.L})
+  for (int* x : {&r.b, &r.first, &r.part, &r.chunks, &r.chunk, &r.tile, &r.head, &r.c0, &r.c1, &r.seq.row0, &r.seq.T, &r.seq.L})
     *x = __builtin_amdgcn_readfirstlane(*x);
   if (it == r.first && tid == 0) {         // for the join
-    a.rec[2 * r.b] = it;
+    a.rec[2 * r.b] = r.part;
     a.rec[2 * r.b + 1] = r.chunks;
   }
-  return true;
+  return r.chunks == 1 || (uint32_t)r.part < (uint32_t)a.parts;   // always: see tree_shape
 }
 
 // One 16-byte piece as bfloat16 into a staged row.
@@ -673,7 +682,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
       if (a.lse && part == 0)
         a.lse[(int64_t)head * a.n_rows + sq.row0 + jtok] = l == 0.0f ? -INFINITY : (m + fast_log2(l)) * LN2;
     } else {
-      const int64_t at = (int64_t)blockIdx.x * ROWS + 16 * n + jr;
+      const int64_t at = (int64_t)it.part * ROWS + 16 * n + jr;
       float* to = a.part_o + at * D + part * 8;
       *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
       *reinterpret_cast<float4*>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
@@ -1238,7 +1247,7 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
     if (WL && h == 0)
       a.lse[(int64_t)head * a.n_rows + sq.row0 + tok] = r.l == 0.0f ? -INFINITY : (r.m + fast_log2(r.l)) * LN2;
   } else {
-    const int64_t at = (int64_t)blockIdx.x * ROWS + 32 * wr + c;
+    const int64_t at = (int64_t)it.part * ROWS + 32 * wr + c;
     float* to = a.part_o + at * D;
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
@@ -1347,7 +1356,7 @@ __device__ __forceinline__ void join_row(const TreeArgs& a, int64_t at0, int64_t
 // A sequence without rows, or (row_start not ascending) behind the items that
 // were launched, has no record: whatever the workspace held is no index.
 __device__ __forceinline__ bool was_cut(const TreeArgs& a, const Seq& s, int first, int chunks, int tiles) {
-  return s.T > 0 && chunks > 1 && first >= 0 && first + (int64_t)chunks * a.c.Hkv * tiles <= a.items;
+  return s.T > 0 && chunks > 1 && first >= 0 && first + (int64_t)chunks * a.c.Hkv * tiles <= a.parts;
 }
 
 template <int ROWS>
@@ -1420,10 +1429,14 @@ TreeShape tree_shape(const mmi_tree& t, int Hkv, int type, int cus) {
   const int64_t limit = (int64_t)1 << 22;
   if (items > limit || (int64_t)t.max_rows * t.Hq * t.n_seq > 2 * limit) throw Error(MMI_ERR_UNSUPPORTED, "the batch is cut into more than 2^22 workgroups");
   s.items = (int32_t)items;
+  // Only cut sequences leave partials. Each is longer than a chunk, so its
+  // chunks are fewer than twice its length in chunks, and a chunk is at least
+  // the batch's work / target: fewer than 2 target of them in all.
+  s.parts = t.max_len <= CHUNK ? 0 : (int32_t)std::min<int64_t>(items, 2 * s.target);
   s.part_o = 0;
-  s.part_ml = up((size_t)items * s.rows * D * 4);
-  s.rec = s.part_ml + up((size_t)items * s.rows * 16);
-  s.bytes = s.rec + up((size_t)t.n_seq * 8);
+  s.part_ml = up((size_t)s.parts * s.rows * D * 4);
+  s.rec = s.part_ml + up((size_t)s.parts * s.rows * 16);
+  s.bytes = s.rec + up((size_t)std::max(t.n_seq, 1) * 8);
   return s;
 }
 

@@ -1684,6 +1684,7 @@ int mmi_tree_attention(mmi_ctx* ctx, const mmi_cache* cache, const mmi_tree* tre
     a.target = s.target;
     a.cus = ctx->cus;
     a.items = s.items;
+    a.parts = s.parts;
     OnDevice d(ctx->device);
     HIPCHK(launch_tree(a, cache->type, s.rows, (hipStream_t)stream));
   });

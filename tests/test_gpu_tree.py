@@ -344,3 +344,36 @@ def test_weights_of_few_rows_keep_15_bits(ctx, kind, T, g, L):
             tol = tol * (1 + HALF_STEP) + HALF_STEP * np.abs(want) + 1e-30
             worst = max(worst, (np.abs(got[i, x] - want) / tol).max())
     assert worst <= 1, worst
+
+
+@pytest.mark.parametrize("n,T,Hq,Hkv", [(1024, 64, 28, 4), (64, 256, 28, 4), (4096, 64, 32, 8), (4096, 1, 32, 8), (1, 1, 2, 1)])
+def test_workspace_of_large_batches(ctx, n, T, Hq, Hkv):
+    """Partials are those of sequences that are cut, fewer than twice the parts that a batch is cut into: at most one
+    a compute unit of 256 rows, or three of 16, each row 128 sums and three numbers (528 bytes with their place)."""
+    from paper_2504_16083_amd import cache as KV
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")  # noqa: E731
+    cache = KV.Cache.empty("fp8", 1, Hkv, 64)
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    for max_len, most in ((1 << 20, 2 * cus * 256 * 528 + 8 * n + 1024), (128, 8 * n + 512)):
+        tree = KV.Tree(i32(n + 1), i32(n), i32(n, max_len // 64), max_rows=T, max_len=max_len)
+        assert 0 < KV.mmi_tree_workspace(ctx, cache, tree, Hq, n * T) <= most
+
+
+@pytest.mark.parametrize("n,T,Hq,Hkv", [(40, 128, 14, 2), (100, 40, 16, 2), (600, 2, 16, 4), (70, 6, 16, 4)])
+def test_partials_of_batches_with_many_tiles(ctx, n, T, Hq, Hkv):
+    """More tiles than workgroups that run at once, a few sequences cut among whole ones: their partials stay in the
+    workspace, and in their places."""
+    from paper_2504_16083_amd import cache as KV
+    rng = np.random.default_rng(n)
+    long = [0, 5, n // 2, n - 3, n - 1]
+    lens = [int(rng.integers(2000, 4000)) if b in long else int(rng.integers(0, 60)) for b in range(n)]
+    drafts = [T if b in long else int(rng.integers(0, T + 1)) for b in range(n)]
+    b = Batch("fp8", lens, drafts, Hq, Hkv, 16, seed=n)
+    size = KV.mmi_tree_workspace(ctx, b.cache, b.tree, Hq, b.n)
+    big = torch.full((size + 8192,), 0xff, dtype=torch.uint8, device="cuda")
+    o, lse = b.outputs()
+    KV.mmi_tree_attention(ctx, b.cache, b.tree, b.q, b.k, b.v, o, big[4096:-4096], lse=lse)
+    assert (big[:4096] == 0xff).all() and (big[-4096:] == 0xff).all()
+    b.check(o, lse, rows={(s, i) for s in [*long, 1, n // 2 + 1] for i in (0, T - 1)})
+    again = b.run(ctx)
+    assert torch.equal(again[0], o) and torch.equal(again[1], lse)

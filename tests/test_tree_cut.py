@@ -15,8 +15,8 @@ MOST = 1 << 30                   # cached tokens of a sequence
 
 @pytest.fixture(scope="module")
 def cut(tmp_path_factory):
-    """cut([(Hkv, target, [(sequences, tiles, tokens)])]) -> [(chunk, items)]: the chunk length of each batch and the
-    items it makes (-1 where the length is not positive)."""
+    """cut([(Hkv, target, [(sequences, tiles, tokens)])]) -> [(chunk, items, cut)]: the chunk length of each batch,
+    the items it makes (-1 where the length is not positive) and those of sequences that are cut."""
     if not shutil.which("g++") or not os.path.exists("/opt/rocm/include/hip/hip_runtime.h"):
         pytest.skip("no host compiler or HIP headers")
     d = tmp_path_factory.mktemp("cut")
@@ -41,7 +41,10 @@ int main() {{
       return s;
     }};
     const int chunk = mmi::choose_chunk(work, all, (int)Hkv, (int)target, count);
-    printf("%d %lld\\n", chunk, chunk > 0 ? count(chunk) * Hkv : -1);
+    long long cut = 0;
+    for (int i = 0; i < n && chunk > 0; ++i)
+      if (L[i] > chunk) cut += k[i] * tiles[i] * mmi::chunks_of((int)L[i], chunk);
+    printf("%d %lld %lld\\n", chunk, chunk > 0 ? count(chunk) * Hkv : -1, cut * Hkv);
   }}
 }}
 ''')
@@ -58,8 +61,8 @@ int main() {{
 
 
 def holds(batches, got):
-    for (Hkv, target, seqs), (chunk, items) in zip(batches, got):
-        what = (Hkv, target, seqs, chunk, items)
+    for (Hkv, target, seqs), (chunk, items, cut) in zip(batches, got):
+        what = (Hkv, target, seqs, chunk, items, cut)
         units = Hkv * sum(n * t for n, t, _ in seqs)
         work = Hkv * sum(n * t * L for n, t, L in seqs)
         assert chunk > 0 and chunk % 128 == 0, what
@@ -68,6 +71,7 @@ def holds(batches, got):
         if units < target:
             assert items <= target, what                         # they all start together
         assert items >= units, what
+        assert cut < 2 * target, what                            # partials of cut sequences
         if units + work // 128 < target:
             assert chunk == 128, what
 
