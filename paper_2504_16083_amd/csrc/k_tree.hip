@@ -316,10 +316,13 @@ __device__ __forceinline__ void add_not_finite(f32x16 (&o)[4], uint16_t* flags, 
 // q = l / 16) holds row r of an operand and 8 of its 32 contracted entries.
 // K comes from the cache straight into that layout (64 contiguous bytes of a
 // row a load; which channels an MFMA contracts does not matter, Q follows);
-// only V goes through LDS, to be read transposed. Three workgroups a compute
-// unit keep about 100 KB of loads in flight. One token over 524288, 32 heads
-// on 8: bfloat16 368 us (5.8 TB/s of cache), E4M3 201 (5.5), int8 233 (4.8),
-// E2M1 112 (5.1); the smaller types wait for the vector ALU that decodes them.
+// only V goes through LDS, to be read transposed. Two or three workgroups a
+// compute unit (tree_shape) keep about 100 KB of loads in flight. One token
+// over 524288, 32 heads on 8: bfloat16 364 us (5.9 TB/s of cache), E4M3 201
+// (5.5), int8 229 (4.9), E2M1 121 (4.7); two tiles, 4 drafts of 7 heads a KV
+// head over 262144: 121 to 125 us (4.3), 59 (4.7), 80 (3.5), 52 (2.7). The
+// smaller types wait for the vector ALU that decodes them and, with two tiles,
+// makes the weights of 32 rows for each of their bytes.
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -692,8 +695,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RN == 1 ? 3
 }
 
 // ------------------------------------------------------------------ many rows
-// With more than 64 rows a head the products, not the cache's bytes, bound the
-// work: keys are staged once for all rows of a workgroup's tile. Its eight
+// With more than 32 rows a head the products, not the cache's bytes, bound the
+// work (up to 64 about both): keys are staged once for all rows of a workgroup's tile. Its eight
 // waves (two a SIMD) are WR groups of 32 rows times 8 / WR groups of keys;
 // the keys go through four LDS stages of 64, one barrier a stage.
 //
@@ -746,7 +749,7 @@ __device__ __forceinline__ const __attribute__((address_space(1))) T* scalar(con
 // a load, and a lane's offset that never changes.
 struct KeySource {
   const int32_t* pages;
-  int head, c0, c1, wave, lane;
+  int head, c1, wave, lane;
   uint32_t zero;                       // in a vector register: keeps the page table's loads vector loads
 };
 
@@ -1000,7 +1003,7 @@ __global__ __launch_bounds__(NTW) __attribute__((amdgpu_waves_per_eu(2))) void k
   const int steps = (it.c1 - it.c0 + WK * SK - 1) / (WK * SK) * WK;
   uint32_t zero = 0;
   asm("" : "+v"(zero));
-  const KeySource src = {a.pages + (int64_t)it.b * a.max_pages, it.head, it.c0, it.c1, wave, lane, zero};
+  const KeySource src = {a.pages + (int64_t)it.b * a.max_pages, it.head, it.c1, wave, lane, zero};
   // Two stages are on their way in registers, in turn: a load has two steps to arrive.
   Raw64<TYPE> even, odd;
   typename Raw64<TYPE>::Ids pid, next;
@@ -1415,9 +1418,11 @@ TreeShape tree_shape(const mmi_tree& t, int Hkv, int type, int cus) {
   const int g = t.Hq / Hkv;
   // what bounds the work changes at 32 rows a head (16 rows: half the softmax
   // and products of 32); a wide workgroup holds a compute unit, three or two
-  // of the few-row ones share it. Two of them read 16-bit rows faster than
-  // three (32 sequences of 8192 tokens and 8 heads: 192 us for 223), three
-  // the smaller rows (E4M3 121 us for 137, E2M1 69 for 84).
+  // of the few-row ones share it. 16-bit rows are read by two (16 sequences of
+  // 20000 tokens, 32 heads on 8, 123 us for 126 with three), smaller ones by
+  // three (32 of 8192: E2M1 63 us for 65 with two, int8 129 for 131, E4M3 110
+  // for 108), 32 rows of any type by two (their registers; E4M3, 4 drafts of 7
+  // heads a KV head over 262144, 59 us for 65).
   const int rows = t.max_rows * g;
   s.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
   s.target = cus * (s.rows > 32 ? 1 : s.rows == 32 || type == MMI_CACHE_BF16 ? 2 : 3);
